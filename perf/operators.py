@@ -1,0 +1,471 @@
+"""Timed cases of the operators around kept chunk caches: attention over a packed prompt, the cache
+held in 4 bits (stored, restored with positions) and the attention that reads it.
+
+Four kinds of pass:
+
+``packed``   ``api.pkv_packed_attn``: causal attention over sequences of different lengths, packed
+             one behind the other - the chunks of a document through one layer.
+``keep``     ``api.pkv_kv4_store`` and ``api.pkv_kv4_restore``: a chunk cache goes into 4 bits and comes
+             back with its positions.
+``fetch``    ``api.pkv_kv4_restore`` alone: the chunks that a request retrieves, from a larger store.
+``answer``   ``api.pkv_kv4_store`` of the new rows and ``api.pkv_kv4_attn`` of them over the whole
+             cache: the attention of one decoding step, for one sequence or a batch.
+
+Where ``own`` is false the same is computed with elementary torch operations in 32 bits.
+
+The 4-bit format: 16 neighbouring elements of a head share the scale 2^e, e = byte - 127; an element
+is one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 times it, with a sign (code = sign * 8 + index), nearest, ties to the even code.  e is
+floor(log2(largest magnitude)) - 2, or one more where the largest magnitude is 7 * 2^e or more.
+"""
+
+from __future__ import annotations
+
+import math
+import random
+
+import torch
+
+own = False
+
+GEOMETRIES = {
+    # heads, kv heads, head size, type, base of the rotary frequencies: as in the configurations
+    # that the library is benchmarked and tested with
+    "f32-4h": (4, 4, 64, "f32", 1e4),
+    "diag-8h": (8, 2, 128, "bf16", 5e5),
+    "llama8b": (32, 8, 128, "bf16", 5e5),
+    "qwen14b": (40, 8, 128, "bf16", 1e6),
+    "bf16-64": (16, 4, 64, "bf16", 1e4),
+}
+SCALE_BYTES = (32, 252)   # range of the scale bytes
+BLOCK = 16                # elements that share a scale
+
+
+def packed(geo, lens, **name):
+    return dict(name, kind="packed", geo=geo, lens=" ".join(map(str, lens)))
+
+
+def keep(geo, rows, **name):
+    return dict(name, kind="keep", geo=geo, rows=rows)
+
+
+def fetch(geo, chunks, chunk_len, stored, **name):
+    return dict(name, kind="fetch", geo=geo, chunks=chunks, chunk_len=chunk_len, stored=stored)
+
+
+def answer(geo, lens, rows_each=1, **name):
+    return dict(name, kind="answer", geo=geo, lens=" ".join(map(str, lens)), rows_each=rows_each)
+
+
+def listed():
+    return [
+        # a few short passages in single precision: launch and latency
+        packed("f32-4h", [1, 96, 143, 60], name="packed f32 300"),
+        # a small model's document, cut at its paragraphs
+        packed("diag-8h", [256, 31, 411, 1, 190, 300, 512, 77, 222], name="packed small model 2k"),
+        # the chunks that one retrieval brings, of about 512 tokens each
+        packed("llama8b", [512, 487, 500, 333, 512, 61, 508, 1], name="packed 8 chunks"),
+        # a batch of whole documents with a long one among them
+        packed("llama8b", [8192, 1023, 4100, 17, 2500, 511, 7001], name="packed 23k"),
+        # a small single-precision cache kept and taken back
+        keep("f32-4h", 700, name="keep f32 700"),
+        # the context of the benchmark's request: 64 chunks of 512 tokens
+        keep("llama8b", 32768, name="keep 32k"),
+        # seven retrieved chunks out of a store of 64, groups of five heads
+        fetch("qwen14b", 7, 512, 32768, name="fetch 7 chunks"),
+        # a decoding step of the small single-precision model
+        answer("f32-4h", [1040], name="answer f32 1k"),
+        # a decoding step behind the benchmark's context
+        answer("llama8b", [32896], name="answer 32k"),
+        # a decoding step behind the longest context
+        answer("llama8b", [131328], name="answer 128k"),
+        # a batch of requests at different points, one slot of it unused
+        answer("qwen14b", [4161, 700, 12033, 1, 2500, 8191, 0, 333, 5000, 6100, 64, 3001, 9000, 1500, 27,
+                           4096], name="answer batch of 16"),
+        # four drafted tokens at once for each of a few requests
+        answer("llama8b", [8200, 16001, 3333, 12000], rows_each=4, name="answer 4 x 4 rows"),
+    ]
+
+
+def log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    most = {}
+    for c in listed():
+        most[c["kind"]] = max(most.get(c["kind"], 0.0), cost(c))
+    while True:
+        kind = rng.choice(["packed", "packed", "packed", "keep", "fetch", "answer", "answer", "answer"])
+        geo = rng.choice(["f32-4h", "diag-8h", "llama8b", "llama8b", "qwen14b", "bf16-64"])
+        f32 = geo == "f32-4h"
+        if kind == "packed":
+            total = log_int(rng, 64, 2048 if f32 else 24000)
+            lens = []
+            while sum(lens) < total and len(lens) < 64:
+                lens.append(min(log_int(rng, 1, max(2, total)), total - sum(lens)))
+            case = packed(geo, lens)
+        elif kind == "keep":
+            case = keep(geo, log_int(rng, 1, 4096 if f32 else 32768))
+        elif kind == "fetch":
+            chunk = log_int(rng, 32, 1024)
+            case = fetch(geo, rng.randint(1, 12), chunk, chunk * rng.randint(12, 40) + rng.randint(0, 9))
+        else:
+            longest = log_int(rng, 64, 4096 if f32 else 131072)
+            lens = [longest] + [log_int(rng, 1, longest) for _ in range(rng.choice([0, 0, 3, 15, 40]))]
+            case = answer(geo, lens, rng.choice([1, 1, 1, 2, 5]))
+            hkv, d = GEOMETRIES[geo][1:3]
+            if len(lens) * longest * hkv * d > 1 << 29:   # the plain form pads the sequences
+                continue
+        if cost(case) <= most[kind]:
+            return case
+
+
+# ---- work ---------------------------------------------------------------------------------
+
+def lens_of(case):
+    return [int(x) for x in case["lens"].split()]
+
+
+def work(case):
+    hq, hkv, d, dtype, _ = GEOMETRIES[case["geo"]]
+    elt = 4 if dtype == "f32" else 2
+    row4 = 2 * hkv * (d // 2 + d // BLOCK)          # a token in 4 bits, keys and values
+    row = 2 * hkv * d * elt                         # the same in the storage type
+    if case["kind"] == "packed":
+        lens = lens_of(case)
+        m = sum(lens)
+        return {"bytes": m * (2 * hq * d * elt + row + 4 * hq + 4),
+                "flops": 4 * d * hq * sum(n * (n + 1) / 2 for n in lens)}
+    if case["kind"] == "keep":
+        return {"bytes": case["rows"] * 2 * (row + row4), "flops": 0}
+    if case["kind"] == "fetch":
+        m = case["chunks"] * case["chunk_len"]
+        return {"bytes": m * (row + row4 + 8), "flops": 0}
+    lens, each = lens_of(case), case["rows_each"]
+    m, keys = len(lens) * each, sum(lens)
+    seen = sum(max(0, n - each + 1 + r) for n in lens for r in range(each))
+    return {"bytes": keys * row4 + m * (row + 2 * hq * d * elt + 4 * hq + 8), "flops": 4 * d * hq * seen}
+
+
+def cost(case):
+    w = work(case)
+    return max(w["bytes"], w["flops"] / 300)
+
+
+# ---- inputs ---------------------------------------------------------------------------------
+
+def quantise(x):
+    """Codes [.., D] and scale bytes [.., D / 16] (uint8) of x."""
+    x = x.float()
+    b = x.unflatten(-1, (-1, BLOCK))
+    frac, power = torch.frexp(b.abs().amax(-1))
+    e = (power - 3 + (frac >= 0.875).int()).clamp(SCALE_BYTES[0] - 127, SCALE_BYTES[1] - 127)
+    y = torch.ldexp(b, -e.unsqueeze(-1))
+    a = y.abs()
+    step = torch.where(a < 2, 0.5, torch.where(a < 4, 1.0, 2.0))
+    a = (torch.round(a / step) * step).clamp(max=6.0)
+    index = torch.where(a <= 2, 2 * a, torch.where(a <= 4, a + 2, a / 2 + 4))
+    codes = (index + torch.where(torch.signbit(y), 8.0, 0.0)).to(torch.uint8)
+    return codes.flatten(-2), (e + 127).to(torch.uint8)
+
+
+def values(codes, scales):
+    """The values that codes [.., D] and scale bytes [.., D / 16] stand for, fp32."""
+    table = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0], device=codes.device)
+    v = table[(codes & 7).int()] * torch.where(codes > 7, -1.0, 1.0)
+    return torch.ldexp(v.unflatten(-1, (-1, BLOCK)), scales.int().unsqueeze(-1) - 127).flatten(-2)
+
+
+def pack(codes):
+    return codes[..., 0::2] | (codes[..., 1::2] << 4)
+
+
+def unpack(bytes_):
+    return torch.stack((bytes_ & 15, bytes_ >> 4), -1).flatten(-2)
+
+
+def kept(k, v, rows):
+    """k, v [n, Hkv, D] as the four tensors of a cache of ``rows`` rows, the first n in use."""
+    n, hkv, d = k.shape
+    out = []
+    for x in (k, v):
+        codes = torch.zeros((hkv, rows, d // 2), dtype=torch.uint8, device=x.device)
+        scales = torch.full((hkv, rows, d // BLOCK), 127, dtype=torch.uint8, device=x.device)
+        c, s = quantise(x.transpose(0, 1))
+        codes[:, :n], scales[:, :n] = pack(c), s
+        out += [codes, scales]
+    out[3] = out[3].view(hkv, rows // 8, 8, d // BLOCK).transpose(2, 3).contiguous()
+    return out
+
+
+def unkept(cache, rows):
+    """Values fp32 [Hkv, *rows.shape, D] of the given cache rows, keys and values."""
+    k_codes, k_scales, v_codes, v_scales = cache
+    hkv, n = k_codes.shape[:2]
+    v_scales = v_scales.transpose(2, 3).reshape(hkv, n, -1)
+    return (values(unpack(k_codes[:, rows]), k_scales[:, rows]),
+            values(unpack(v_codes[:, rows]), v_scales[:, rows]))
+
+
+def prepare(case, seed):
+    hq, hkv, d, dtype, theta = GEOMETRIES[case["geo"]]
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    dev = "cuda"
+    gen = torch.Generator(device=dev).manual_seed(seed)
+    new = lambda *shape: torch.randn(shape, generator=gen, device=dev).to(dt)  # noqa: E731
+    i32 = dict(dtype=torch.int32, device=dev)
+    s = dict(case, heads=(hq, hkv, d), dt=dt, theta=theta)
+    if case["kind"] == "packed":
+        lens = lens_of(case)
+        m = sum(lens)
+        s.update(q=new(m, hq, d), k=new(m, hkv, d), v=new(m, hkv, d), seq=lens)
+        s["pos"] = torch.cat([torch.arange(n, **i32) for n in lens])
+        s["out"], s["lse"] = torch.empty_like(s["q"]), torch.empty((m, hq), device=dev)
+    elif case["kind"] == "answer":
+        lens, each = lens_of(case), case["rows_each"]
+        m, total = len(lens) * each, sum(lens)
+        s["start"] = torch.tensor([sum(lens[:i]) for i in range(len(lens))], **i32)
+        n = torch.tensor(lens, **i32).unsqueeze(1)
+        # row r of a sequence sits each - 1 - r rows in front of its end; a slot without tokens
+        # attends nothing and its row goes behind all others
+        r = torch.arange(each, **i32).unsqueeze(0)
+        s["pos"] = (n - each + r).clamp(min=-1).flatten()
+        rows = -(-(total + m) // 32) * 32
+        spare = total + torch.arange(m, **i32)
+        s["dst"] = torch.where(s["pos"] >= 0, s["start"].repeat_interleave(each) + s["pos"], spare)
+        s["cache"] = kept(new(total, hkv, d), new(total, hkv, d), rows)
+        s.update(q=new(m, hq, d), k=new(m, hkv, d), v=new(m, hkv, d), seq=lens)
+        s["out"], s["lse"] = torch.empty_like(s["q"]), torch.empty((m, hq), device=dev)
+    else:
+        if case["kind"] == "keep":
+            m, rows = case["rows"], -(-case["rows"] // 32) * 32
+            s.update(k=new(m, hkv, d), v=new(m, hkv, d))
+            s["cache"] = [torch.zeros((hkv, rows, d // 2), dtype=torch.uint8, device=dev),
+                          torch.zeros((hkv, rows, d // BLOCK), dtype=torch.uint8, device=dev),
+                          torch.zeros((hkv, rows, d // 2), dtype=torch.uint8, device=dev),
+                          torch.zeros((hkv, rows // 8, d // BLOCK, 8), dtype=torch.uint8, device=dev)]
+        else:
+            n, rows = case["stored"], -(-case["stored"] // 32) * 32
+            m = case["chunks"] * case["chunk_len"]
+            s["cache"] = kept(new(n, hkv, d), new(n, hkv, d), rows)
+            chunks = random.Random(seed).sample(range(n // case["chunk_len"]), case["chunks"])
+            s["rows"] = torch.cat([torch.arange(c * case["chunk_len"], (c + 1) * case["chunk_len"], **i32)
+                                   for c in chunks])
+        s["k_out"], s["v_out"] = (torch.empty((m, hkv, d), dtype=dt, device=dev) for _ in range(2))
+        s["pos"] = torch.arange(m, **i32)
+    if own:   # what a program makes once: the library's view of the cache, its workspace
+        from paper_2602_02579_amd import api
+        s["cfg"] = cfg = api.LayerCfg(hq, hkv, d, hq * d, theta, dtype)
+        if "cache" in s:
+            s["cache"] = api.Kv4Cache(cfg, *s["cache"])
+        need = 0
+        if case["kind"] == "packed":
+            need = api.pkv_packed_attn_workspace_bytes(cfg, m)
+        elif case["kind"] == "answer":
+            need = api.pkv_kv4_attn_workspace_bytes(cfg, s["cache"].rows, m, len(lens))
+        s["ws"] = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+    return s
+
+
+# ---- the operators ------------------------------------------------------------------------
+
+def turn(x, pos, theta):
+    """x [n, heads, D] (fp32) turned by its positions: element i with i + D / 2."""
+    half = x.shape[-1] // 2
+    freq = theta ** (-torch.arange(half, dtype=torch.float64, device=x.device) / half)
+    angle = pos.double().unsqueeze(1) * freq
+    c, s = angle.cos().float().unsqueeze(1), angle.sin().float().unsqueeze(1)
+    a, b = x[..., :half], x[..., half:]
+    return torch.cat((a * c - b * s, b * c + a * s), -1)
+
+
+def softmax_rows(scores, seen):
+    """Weights and normalisers along the last axis over what is seen; rows that see nothing: 0, -inf."""
+    scores = scores.masked_fill(~seen, float("-inf"))
+    top = scores.amax(-1, keepdim=True)
+    top = torch.where(torch.isinf(top), 0.0, top)
+    p = torch.exp(scores - top)
+    total = p.sum(-1, keepdim=True)
+    return p / torch.where(total > 0, total, 1.0), (top + torch.log(total)).squeeze(-1)
+
+
+BLOCK_ROWS = 2048   # rows whose scores are held at once
+
+
+def run(s):
+    if own:
+        from paper_2602_02579_amd import api
+        if s["kind"] == "packed":
+            api.pkv_packed_attn(s["cfg"], s["q"], s["k"], s["v"], s["pos"], s["out"], s["lse"], ws=s["ws"])
+            return s["out"], s["lse"]
+        if s["kind"] == "answer":
+            api.pkv_kv4_store(s["cfg"], s["k"], s["v"], s["cache"], s["dst"])
+            api.pkv_kv4_attn(s["cfg"], s["q"], s["cache"], s["pos"], s["out"], s["start"], len(s["seq"]),
+                             s["lse"], ws=s["ws"])
+            return s["out"], s["lse"]
+        if s["kind"] == "keep":
+            api.pkv_kv4_store(s["cfg"], s["k"], s["v"], s["cache"])
+        api.pkv_kv4_restore(s["cfg"], s["cache"], s["k_out"], s["v_out"], s.get("rows"), s["pos"])
+        return s["k_out"], s["v_out"]
+
+    hq, hkv, d = s["heads"]
+    group, scale = hq // hkv, 1.0 / math.sqrt(d)
+    if s["kind"] == "packed":
+        m = s["q"].shape[0]
+        q = s["q"].float().view(m, hkv, group, d).permute(1, 2, 0, 3)
+        k, v = (s[n].float().transpose(0, 1).unsqueeze(1) for n in "kv")
+        at = torch.arange(m, device=q.device)
+        first = at - s["pos"]
+        for r0 in range(0, m, BLOCK_ROWS):   # keys: from where the block's first row's sequence begins
+            r1 = min(m, r0 + BLOCK_ROWS)
+            k0 = begin(s["seq"], r0)
+            keys = at[k0:r1]
+            seen = (keys >= first[r0:r1, None]) & (keys <= at[r0:r1, None])
+            p, lse = softmax_rows((q[:, :, r0:r1] @ k[:, :, k0:r1].transpose(-1, -2)) * scale, seen)
+            s["out"][r0:r1] = (p @ v[:, :, k0:r1]).permute(2, 0, 1, 3).reshape(r1 - r0, hq, d).to(s["dt"])
+            s["lse"][r0:r1] = lse.permute(2, 0, 1).reshape(r1 - r0, hq)
+        return s["out"], s["lse"]
+    if s["kind"] == "answer":
+        cache, each, longest = s["cache"], s["rows_each"], max(s["seq"])
+        for i, x in ((0, s["k"]), (2, s["v"])):
+            codes, scales = quantise(x.transpose(0, 1))
+            dst = s["dst"].long()
+            cache[i][:, dst] = pack(codes)
+            if i == 0:
+                cache[1][:, dst] = scales
+            else:
+                cache[3][:, dst // 8, :, dst % 8] = scales.transpose(0, 1)
+        n = len(s["seq"])
+        at = torch.arange(longest, device=dst.device)
+        rows = (s["start"].unsqueeze(1) + at).clamp(max=cache[0].shape[1] - 1)
+        k, v = unkept(cache, rows.long())                       # [Hkv, n, longest, D]
+        q = s["q"].float().view(n, each, hkv, group, d).permute(2, 0, 1, 3, 4).flatten(2, 3)
+        seen = (at <= s["pos"].view(n, each, 1)).repeat_interleave(group, 1)
+        p, lse = softmax_rows((q @ k.transpose(-1, -2)) * scale, seen)
+        s["out"][:] = (p @ v).view(hkv, n, each, group, d).permute(1, 2, 0, 3, 4).reshape(-1, hq, d).to(s["dt"])
+        s["lse"][:] = lse.view(hkv, n, each, group).permute(1, 2, 0, 3).reshape(-1, hq)
+        return s["out"], s["lse"]
+    if s["kind"] == "keep":
+        m = s["k"].shape[0]
+        k, v = (values(*quantise(s[n])) for n in "kv")
+    else:
+        k, v = (x.transpose(0, 1) for x in unkept(s["cache"], s["rows"].long()))
+    s["k_out"][:] = turn(k, s["pos"], s["theta"]).to(s["dt"])
+    s["v_out"][:] = v.to(s["dt"])
+    return s["k_out"], s["v_out"]
+
+
+def begin(lens, row):
+    """Where the sequence that holds a packed row begins."""
+    at = 0
+    for n in lens:
+        if at + n > row:
+            return at
+        at += n
+    return at
+
+
+# ---- the definitions in 64 bits -------------------------------------------------------------
+
+def kept_values(x):
+    """What 4 bits keep of x [.., D], in fp64: for every element the nearest of the 15 values."""
+    x = x.double().unflatten(-1, (-1, BLOCK))
+    top = x.abs().amax(-1, keepdim=True)
+    _, power = torch.frexp(top)
+    e = (power - 3).double()
+    e = torch.where(top >= 7 * torch.exp2(e), e + 1, e).clamp(SCALE_BYTES[0] - 127, SCALE_BYTES[1] - 127)
+    unit = torch.exp2(e)
+    size = (x / unit).abs()
+    out = torch.zeros_like(size)
+    # past the middle of two values the upper one; in the middle the one with the even code
+    for low, high, even_is_high in ((0, .5, False), (.5, 1, True), (1, 1.5, False), (1.5, 2, True),
+                                    (2, 3, False), (3, 4, True), (4, 6, False)):
+        middle = (low + high) / 2
+        past = (size >= middle) if even_is_high else (size > middle)
+        out = torch.where(past, float(high), out)
+    return (torch.copysign(out, x) * unit).flatten(-2)
+
+
+def attend(q, k, v, positions, scale):
+    """q [r, Hq, D] over k, v [n, Hkv, D] (fp64); row i sees the keys up to positions[i]."""
+    r, hq, d = q.shape
+    n, hkv = k.shape[:2]
+    out = torch.zeros(r, hq, d, dtype=torch.float64, device=q.device)
+    lse = torch.full((r, hq), float("-inf"), dtype=torch.float64, device=q.device)
+    for r0 in range(0, r, 1024):
+        some = positions[r0:r0 + 1024]
+        most = min(n, int(some.max()) + 1)
+        if most <= 0:
+            continue
+        hidden = torch.arange(most, device=q.device) > some.unsqueeze(1)
+        for h in range(hq):
+            g = h // (hq // hkv)
+            z = torch.mm(q[r0:r0 + 1024, h], k[:most, g].t().contiguous()) * scale
+            z[hidden] = float("-inf")
+            norm = torch.logsumexp(z, -1)
+            lse[r0:r0 + 1024, h] = norm
+            w = torch.exp(z - norm.unsqueeze(1))
+            w[hidden] = 0.0
+            out[r0:r0 + 1024, h] = torch.mm(w, v[:most, g].contiguous())
+    return out, lse
+
+
+def stored_values(cache, rows):
+    """Values in fp64 [n, Hkv, D] of cache rows, straight from the layout."""
+    k_codes, k_scales, v_codes, v_scales = cache
+    size = torch.tensor([0, .5, 1, 1.5, 2, 3, 4, 6], dtype=torch.float64, device=rows.device)
+    size = torch.cat((size, -size))
+    both = []
+    for codes, byte in ((k_codes, k_scales[:, rows]), (v_codes, v_scales[:, rows // 8, :, rows % 8].transpose(0, 1))):
+        b = codes[:, rows].long()
+        x = torch.empty(*b.shape[:2], 2 * b.shape[2], dtype=torch.float64, device=rows.device)
+        x[..., 0::2], x[..., 1::2] = size[b % 16], size[b // 16]
+        unit = torch.exp2(byte.double() - 127)
+        both.append((x * unit.repeat_interleave(BLOCK, -1)).transpose(0, 1))
+    return both
+
+
+def rotated(x, pos, theta):
+    d = x.shape[-1]
+    freq = torch.tensor([theta ** (-2.0 * i / d) for i in range(d // 2)], dtype=torch.float64, device=x.device)
+    z = torch.complex(x[..., :d // 2].contiguous(), x[..., d // 2:].contiguous())
+    angle = (pos.double()[:, None] * freq)[:, None, :]
+    z = z * torch.polar(torch.ones_like(angle), angle)
+    return torch.cat((z.real, z.imag), -1)
+
+
+def exact(case, seed):
+    global own
+    was, own = own, False
+    try:
+        s = prepare(case, seed)
+    finally:
+        own = was
+    scale = 1.0 / math.sqrt(s["heads"][2])
+    if case["kind"] == "packed":
+        outs, lses, at = [], [], 0
+        for n in s["seq"]:
+            q, k, v = (s[x][at:at + n].double() for x in "qkv")
+            o, l = attend(q, k, v, torch.arange(n, device=q.device), scale)
+            outs.append(o)
+            lses.append(l)
+            at += n
+        return torch.cat(outs), torch.cat(lses)
+    if case["kind"] == "answer":
+        outs, lses, each = [], [], case["rows_each"]
+        new_k, new_v = kept_values(s["k"]), kept_values(s["v"])
+        for i, n in enumerate(s["seq"]):
+            mine = slice(i * each, (i + 1) * each)
+            k, v = stored_values(s["cache"], s["start"][i].long() + torch.arange(n, device="cuda"))
+            there = s["pos"][mine] >= 0
+            k[s["pos"][mine][there].long()] = new_k[mine][there]
+            v[s["pos"][mine][there].long()] = new_v[mine][there]
+            o, l = attend(s["q"][mine].double(), k, v, s["pos"][mine], scale)
+            outs.append(o)
+            lses.append(l)
+        return torch.cat(outs), torch.cat(lses)
+    if case["kind"] == "keep":
+        k, v = kept_values(s["k"]), kept_values(s["v"])
+    else:
+        k, v = stored_values(s["cache"], s["rows"].long())
+    return rotated(k, s["pos"], s["theta"]), v
