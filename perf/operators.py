@@ -5,10 +5,10 @@ Four kinds of pass:
 
 ``packed``   ``api.pkv_packed_attn``: causal attention over sequences of different lengths, packed
              one behind the other - the chunks of a document through one layer.
-``keep``     ``api.pkv_kv4_store`` and ``api.pkv_kv4_restore``: a chunk cache goes into 4 bits and comes
+``keep``     ``api.pkv_qcache_store`` and ``api.pkv_qcache_restore``: a chunk cache goes into 4 bits and comes
              back with its positions.
-``fetch``    ``api.pkv_kv4_restore`` alone: the chunks that a request retrieves, from a larger store.
-``answer``   ``api.pkv_kv4_store`` of the new rows and ``api.pkv_kv4_attn`` of them over the whole
+``fetch``    ``api.pkv_qcache_restore`` alone: the chunks that a request retrieves, from a larger store.
+``answer``   ``api.pkv_qcache_store`` of the new rows and ``api.pkv_qcache_attn`` of them over the whole
              cache: the attention of one decoding step, for one sequence or a batch.
 
 Where ``own`` is false the same is computed with elementary torch operations in 32 bits.
@@ -257,12 +257,12 @@ def prepare(case, seed):
         from paper_2602_02579_amd import api
         s["cfg"] = cfg = api.LayerCfg(hq, hkv, d, hq * d, theta, dtype)
         if "cache" in s:
-            s["cache"] = api.Kv4Cache(cfg, *s["cache"])
+            s["cache"] = api.QCache(cfg, *s["cache"])
         need = 0
         if case["kind"] == "packed":
             need = api.pkv_packed_attn_workspace_bytes(cfg, m)
         elif case["kind"] == "answer":
-            need = api.pkv_kv4_attn_workspace_bytes(cfg, s["cache"].rows, m, len(lens))
+            need = api.pkv_qcache_attn_workspace_bytes(cfg, s["cache"].rows, m, len(lens))
         s["ws"] = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
     return s
 
@@ -299,13 +299,13 @@ def run(s):
             api.pkv_packed_attn(s["cfg"], s["q"], s["k"], s["v"], s["pos"], s["out"], s["lse"], ws=s["ws"])
             return s["out"], s["lse"]
         if s["kind"] == "answer":
-            api.pkv_kv4_store(s["cfg"], s["k"], s["v"], s["cache"], s["dst"])
-            api.pkv_kv4_attn(s["cfg"], s["q"], s["cache"], s["pos"], s["out"], s["start"], len(s["seq"]),
+            api.pkv_qcache_store(s["cfg"], s["k"], s["v"], s["cache"], s["dst"])
+            api.pkv_qcache_attn(s["cfg"], s["q"], s["cache"], s["pos"], s["out"], s["start"], len(s["seq"]),
                              s["lse"], ws=s["ws"])
             return s["out"], s["lse"]
         if s["kind"] == "keep":
-            api.pkv_kv4_store(s["cfg"], s["k"], s["v"], s["cache"])
-        api.pkv_kv4_restore(s["cfg"], s["cache"], s["k_out"], s["v_out"], s.get("rows"), s["pos"])
+            api.pkv_qcache_store(s["cfg"], s["k"], s["v"], s["cache"])
+        api.pkv_qcache_restore(s["cfg"], s["cache"], s["k_out"], s["v_out"], s.get("rows"), s["pos"])
         return s["k_out"], s["v_out"]
 
     hq, hkv, d = s["heads"]
