@@ -360,6 +360,113 @@ pkv_status pkv_chunk_attn(const pkv_layer_cfg* cfg,
 size_t pkv_chunk_attn_workspace_bytes(const pkv_layer_cfg* cfg, int64_t m, int64_t chunk_len);
 
 /*
+ * Causal attention over a packed prompt: sequences of different lengths, one behind the other in q, k
+ * and v (paper: Sec. 2 - the method's input are chunks prefilled one by one; documents are
+ * not cut into equal ones).  row_pos[i] is the position of row i inside its own sequence, and
+ * tells the packing: row i attends the row_pos[i] + 1 rows that end with itself,
+ *     out[i, h] = sum_{i - row_pos[i] <= t <= i} softmax_t(q[i,h] . k[t,g(h)] * scale) * v[t, g(h)].
+ * A row with row_pos[i] < 0 attends nothing (padding): out 0, lse -inf.  Positions beyond i count
+ * as i, so any value is safe; positions that do not begin anew (a window of w rows: min(pos, w - 1))
+ * are as good.  fp32 softmax and accumulation, one rounding to cfg->dtype.  lse_out, if not NULL,
+ * receives the natural-log normaliser per (row, head).  out may be q itself and overlaps no
+ * other operand.  softmax_scale == 0 means 1/sqrt(D).  All tensors 16-byte aligned
+ * (PKV_ERR_UNSUPPORTED otherwise).  Scratch: pkv_packed_attn_workspace_bytes.  m == 0 is a no-op.
+ */
+pkv_status pkv_packed_attn(const pkv_layer_cfg* cfg,
+                           const void* q,          /* [m, Hq, D] */
+                           const void* k,          /* [m, Hkv, D] */
+                           const void* v,          /* [m, Hkv, D] */
+                           const int32_t* row_pos, /* [m] */
+                           void* out,              /* [m, Hq, D] */
+                           float* lse_out,         /* [m, Hq] or NULL */
+                           int64_t m, float softmax_scale, void* ws, size_t ws_bytes,
+                           void* stream);
+
+size_t pkv_packed_attn_workspace_bytes(const pkv_layer_cfg* cfg, int64_t m);
+
+/*
+ * ---- A cache held in 4 bits ---------------------------------------------
+ *
+ * Keys and values of `rows` tokens in 4.5 bits an element, for chunk caches that are kept until
+ * a request retrieves them, and for the cache that an answer is decoded over (the paper keeps its
+ * caches in the model's type; the format is this library's).  16 neighbouring elements of a
+ * head share a scale 2^(byte - 127); an element is 0, 0.5, 1, 1.5, 2, 3, 4 or 6 times it, with a sign:
+ * code = 8 * (negative) + index in that list, the element with the even index in the low half of
+ * its byte.  pkv_qcache_store writes scale bytes 32 .. 252 and, for 16 elements of which one
+ * is not finite, 255: their values are then NaN.
+ *
+ * The struct is a HOST struct, read during the call; its members are device pointers, 16-byte
+ * aligned (PKV_ERR_UNSUPPORTED otherwise).  rows is a positive multiple of 32.  Key and value
+ * scales are laid out differently: a value's scale lies beside those of the same 16 elements of
+ * its seven neighbours (tokens 8 j .. 8 j + 7), which the attention multiplies together.
+ */
+typedef struct {
+    void* k_codes;    /* uint8 [Hkv, rows, D / 2] */
+    void* k_scales;   /* uint8 [Hkv, rows, D / 16] */
+    void* v_codes;    /* uint8 [Hkv, rows, D / 2] */
+    void* v_scales;   /* uint8 [Hkv, rows / 8, D / 16, 8] */
+    int64_t rows;
+} pkv_qcache;
+
+/*
+ * Keys and values of m tokens into rows dst_row[i] of the cache (NULL: rows 0 .. m - 1).  Every
+ * element becomes the nearest value of the format (ties: the even index), with the scale 2^e, e =
+ * floor(log2(largest magnitude of the 16)) - 2, one more where that magnitude is 7 * 2^e or more,
+ * and within the bytes above: the error is at most half the distance of the two values around it.
+ * dst_row values must be distinct; rows outside the cache are skipped, no other row is touched.
+ * k and v 16-byte aligned.  m == 0 is a no-op.
+ */
+pkv_status pkv_qcache_store(const pkv_layer_cfg* cfg,
+                            const void* k,          /* [m, Hkv, D] */
+                            const void* v,          /* [m, Hkv, D] */
+                            const int32_t* dst_row, /* [m] or NULL */
+                            const pkv_qcache* cache, int64_t m, void* stream);
+
+/*
+ * The way back, into caches of cfg->dtype: k_out[i] = R(p_i) K[r_i], v_out[i] = V[r_i], where r_i
+ * = row_idx ? row_idx[i] : i and p_i = pos ? pos[i] : pos_base + i: retrieved chunks are put
+ * together with their positions, as pkv_rope_restore does for caches in cfg->dtype.  rotate == 0:
+ * keys as they were stored (pos is not read).  The stored values are exact in bf16 and fp32; a
+ * rotated key is rounded once.  Rows outside the cache are skipped (their output rows stay as
+ * they were); the same row may be taken several times.  k_out and v_out 16-byte aligned.
+ * m == 0 is a no-op.
+ */
+pkv_status pkv_qcache_restore(const pkv_layer_cfg* cfg, const pkv_qcache* cache,
+                              const int32_t* row_idx, /* [m] or NULL */
+                              const int32_t* pos,     /* [m] or NULL */
+                              int64_t pos_base, int rotate,
+                              void* k_out,            /* [m, Hkv, D] */
+                              void* v_out,            /* [m, Hkv, D] */
+                              int64_t m, void* stream);
+
+/*
+ * Attention over a cache held in 4 bits: the rows of a decoding step, of one sequence or of
+ * n_seq of them, m / n_seq rows each.  Row i belongs to sequence s = i / (m / n_seq), whose tokens
+ * are the cache rows from seq_start[s] on (NULL: every sequence begins at row 0), and
+ *     out[i, h] = sum_{t <= row_pos[i]} softmax_t(q[i,h] . K[seq_start[s] + t, g(h)] * scale)
+ *                 * V[seq_start[s] + t, g(h)].
+ * row_pos[i] < 0: the row attends nothing (an unused slot): out 0, lse -inf.  Rows outside the
+ * cache are never read: a sequence ends where the cache does.  Sequences may share rows.
+ * q, out and lse_out as in pkv_sparse_row_attn (out may be q itself); 16-byte aligned.  fp32
+ * softmax and accumulation, one rounding to cfg->dtype.  Meant for few rows a sequence (up to
+ * some 64 (row, head of a group) pairs the cache is what is read; beyond, restore it once and use
+ * pkv_sparse_row_attn).  n_seq >= 1 divides m.  Deterministic.  Scratch:
+ * pkv_qcache_attn_workspace_bytes.  m == 0 is a no-op.
+ */
+pkv_status pkv_qcache_attn(const pkv_layer_cfg* cfg,
+                           const void* q,            /* [m, Hq, D] */
+                           const pkv_qcache* cache,
+                           const int32_t* row_pos,   /* [m] */
+                           const int32_t* seq_start, /* [n_seq] or NULL */
+                           void* out,                /* [m, Hq, D] */
+                           float* lse_out,           /* [m, Hq] or NULL */
+                           int64_t m, int64_t n_seq, float softmax_scale,
+                           void* ws, size_t ws_bytes, void* stream);
+
+size_t pkv_qcache_attn_workspace_bytes(const pkv_layer_cfg* cfg, int64_t rows, int64_t m,
+                                       int64_t n_seq);
+
+/*
  * Fused variants for the first stage (paper: Sec. 4.2 - the user query is run through
  * the model against the imprecise cache, and its attention to the context is the value
  * function; Algorithm 1, first stage).  The query rows' attention pass and the score

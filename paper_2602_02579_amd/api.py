@@ -25,7 +25,9 @@ __all__ = ["LayerCfg", "PkvError", "load_library", "library_path",
            "pkv_topk_select", "pkv_gather_qkv_proj", "pkv_gather_qkv_proj_ex",
            "pkv_gather_qkv_proj_scatter", "pkv_scatter_kv",
            "pkv_sparse_row_attn", "pkv_sparse_row_attn_kernel", "pkv_chunk_attn",
-           "pkv_chunk_attn_workspace_bytes",
+           "pkv_chunk_attn_workspace_bytes", "pkv_packed_attn",
+           "pkv_packed_attn_workspace_bytes", "QCache", "pkv_qcache_store", "pkv_qcache_restore",
+           "pkv_qcache_attn", "pkv_qcache_attn_workspace_bytes",
            "pkv_rmsnorm_rows", "pkv_gather_rows", "pkv_linear_rows", "pkv_swiglu_rows",
            "LayerCall", "pkv_layer_rows", "pkv_glue_workspace_bytes",
            "pkv_workspace_bytes", "pkv_status_string", "pkv_version",
@@ -45,6 +47,8 @@ EXPORTED_SYMBOLS = [
     "pkv_sparse_row_attn_ctx_lse_workspace_bytes", "pkv_chunk_attn",
     "pkv_chunk_attn_workspace_bytes", "pkv_layer_rows", "pkv_rope_restore_layers",
     "pkv_sparse_row_attn_kernel", "pkv_workspace_bytes", "pkv_status_string", "pkv_version",
+    "pkv_packed_attn", "pkv_packed_attn_workspace_bytes", "pkv_qcache_store",
+    "pkv_qcache_restore", "pkv_qcache_attn", "pkv_qcache_attn_workspace_bytes",
 ]
 
 
@@ -79,6 +83,12 @@ class _CCfg(ctypes.Structure):
     _fields_ = [("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
                 ("head_dim", ctypes.c_int32), ("hidden", ctypes.c_int32),
                 ("rope_theta", ctypes.c_float), ("dtype", ctypes.c_int32)]
+
+
+class _CQCache(ctypes.Structure):
+    _fields_ = [("k_codes", ctypes.c_void_p), ("k_scales", ctypes.c_void_p),
+                ("v_codes", ctypes.c_void_p), ("v_scales", ctypes.c_void_p),
+                ("rows", ctypes.c_int64)]
 
 
 @dataclass(frozen=True)
@@ -167,6 +177,17 @@ def load_library() -> ctypes.CDLL:
     lib.pkv_sparse_row_attn_kernel.restype = ctypes.c_int32
     lib.pkv_chunk_attn_workspace_bytes.argtypes = [cfgp, i64, i64]
     lib.pkv_chunk_attn_workspace_bytes.restype = ctypes.c_size_t
+    qcp = ctypes.POINTER(_CQCache)
+    lib.pkv_packed_attn.argtypes = [cfgp, vp, vp, vp, i32p, vp, f32p, i64, ctypes.c_float, vp,
+                                    ctypes.c_size_t, vp]
+    lib.pkv_packed_attn_workspace_bytes.argtypes = [cfgp, i64]
+    lib.pkv_qcache_store.argtypes = [cfgp, vp, vp, i32p, qcp, i64, vp]
+    lib.pkv_qcache_restore.argtypes = [cfgp, qcp, i32p, i32p, i64, ctypes.c_int, vp, vp, i64, vp]
+    lib.pkv_qcache_attn.argtypes = [cfgp, vp, qcp, i32p, i32p, vp, f32p, i64, i64,
+                                    ctypes.c_float, vp, ctypes.c_size_t, vp]
+    lib.pkv_qcache_attn_workspace_bytes.argtypes = [cfgp, i64, i64, i64]
+    for name in ("pkv_packed_attn_workspace_bytes", "pkv_qcache_attn_workspace_bytes"):
+        getattr(lib, name).restype = ctypes.c_size_t
     i32 = ctypes.c_int32
     lib.pkv_rmsnorm_rows.argtypes = [i32, vp, i32p, vp, ctypes.c_float, vp, i64, i64, vp]
     lib.pkv_gather_rows.argtypes = [i32, vp, i32p, vp, i64, i64, vp]
@@ -182,7 +203,8 @@ def load_library() -> ctypes.CDLL:
                  "pkv_gather_qkv_proj_scatter", "pkv_scatter_kv",
                  "pkv_sparse_row_attn", "pkv_chunk_attn", "pkv_rmsnorm_rows", "pkv_gather_rows",
                  "pkv_linear_rows", "pkv_swiglu_rows", "pkv_layer_rows",
-                 "pkv_rope_restore_layers"):
+                 "pkv_rope_restore_layers", "pkv_packed_attn", "pkv_qcache_store",
+                 "pkv_qcache_restore", "pkv_qcache_attn"):
         getattr(lib, name).restype = ctypes.c_int
     lib.pkv_workspace_bytes.argtypes = [ctypes.c_int, cfgp, i64, i64]
     lib.pkv_workspace_bytes.restype = ctypes.c_size_t
@@ -553,6 +575,139 @@ def pkv_query_score_lse(cfg: LayerCfg, q: torch.Tensor, k: torch.Tensor, lse: to
         _ptr(lse, torch.float32, "lse"), _ptr(row_pos, torch.int32, "row_pos"),
         _ptr(score, torch.float32, "score"), nq, n_ctx, float(softmax_scale),
         int(bool(accumulate)), wp, wb, _stream()))
+
+
+# ---- packed prompts, the cache in 4 bits -------------------------------------------
+
+def _current(*tensors: Optional[torch.Tensor]) -> None:
+    """The calls run on the current device: their tensors have to be its own."""
+    devices = {t.get_device() for t in tensors if t is not None}
+    if devices != {torch.cuda.current_device()}:
+        raise ValueError("all tensors must be on the current device")
+
+
+def pkv_packed_attn_workspace_bytes(cfg: LayerCfg, m: int) -> int:
+    return int(load_library().pkv_packed_attn_workspace_bytes(cfg._ref, int(m)))
+
+
+def pkv_packed_attn(cfg: LayerCfg, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                    row_pos: torch.Tensor, out: torch.Tensor,
+                    lse_out: Optional[torch.Tensor] = None, softmax_scale: float = 0.0,
+                    ws: Optional[torch.Tensor] = None) -> None:
+    m, dt = row_pos.shape[0], cfg.torch_dtype
+    if row_pos.dim() != 1 or q.shape != (m, cfg.n_q_heads, cfg.head_dim) or out.shape != q.shape:
+        raise ValueError("q/out must be [m, Hq, D], row_pos [m]")
+    if k.shape != (m, cfg.n_kv_heads, cfg.head_dim) or v.shape != k.shape:
+        raise ValueError("k/v must be [m, Hkv, D]")
+    if lse_out is not None and lse_out.shape != (m, cfg.n_q_heads):
+        raise ValueError("lse_out must be [m, Hq]")
+    ptrs = (_ptr(q, dt, "q"), _ptr(k, dt, "k"), _ptr(v, dt, "v"),
+            _ptr(row_pos, torch.int32, "row_pos"), _ptr(out, dt, "out"),
+            _ptr(lse_out, torch.float32, "lse_out"))
+    wp, wb = _ws(ws)
+    _current(q, k, v, row_pos, out, lse_out, ws)
+    _check("pkv_packed_attn", load_library().pkv_packed_attn(
+        cfg._ref, *ptrs, m, float(softmax_scale), wp, wb, _stream()))
+
+
+class QCache:
+    """Keys and values of ``rows`` tokens in 4 bits (``pkv_qcache``): the library's view of four
+    uint8 tensors, which it keeps.  ``k_codes, v_codes [Hkv, rows, D / 2]``, ``k_scales [Hkv, rows,
+    D / 16]``, ``v_scales [Hkv, rows / 8, D / 16, 8]``; ``rows`` a multiple of 32."""
+
+    def __init__(self, cfg: LayerCfg, k_codes: torch.Tensor, k_scales: torch.Tensor,
+                 v_codes: torch.Tensor, v_scales: torch.Tensor):
+        self.heads, self.head_dim = cfg.n_kv_heads, cfg.head_dim
+        self.rows = k_codes.shape[1] if k_codes.dim() == 3 else 0
+        if self.rows <= 0 or self.rows % 32:
+            raise ValueError("the rows of a cache must be a positive multiple of 32")
+        self.tensors = dict(k_codes=k_codes, k_scales=k_scales, v_codes=v_codes,
+                            v_scales=v_scales)
+        for name, shape in self._shapes(cfg, self.rows).items():
+            if self.tensors[name].shape != shape:
+                raise ValueError(f"{name} must be {list(shape)}")
+        self._c = _CQCache(*(_ptr(t, torch.uint8, name) for name, t in self.tensors.items()),
+                           self.rows)
+        if len({t.get_device() for t in self.tensors.values()}) != 1:
+            raise ValueError("all tensors of a cache must be on one device")
+        self._ref = ctypes.byref(self._c)
+
+    @staticmethod
+    def _shapes(cfg: LayerCfg, rows: int):
+        h, d = cfg.n_kv_heads, cfg.head_dim
+        return dict(k_codes=(h, rows, d // 2), k_scales=(h, rows, d // 16),
+                    v_codes=(h, rows, d // 2), v_scales=(h, rows // 8, d // 16, 8))
+
+    @classmethod
+    def empty(cls, cfg: LayerCfg, rows: int, device: torch.device) -> "QCache":
+        """Room for at least ``rows`` tokens, all of them zero."""
+        shapes = cls._shapes(cfg, -(-int(rows) // 32) * 32)
+        return cls(cfg, *(torch.zeros(s, dtype=torch.uint8, device=device)
+                          for s in shapes.values()))
+
+
+def _of_cache(cfg: LayerCfg, cache: QCache) -> torch.Tensor:
+    if (cache.heads, cache.head_dim) != (cfg.n_kv_heads, cfg.head_dim):
+        raise ValueError("the cache was made for other heads")
+    return cache.tensors["k_codes"]
+
+
+def pkv_qcache_store(cfg: LayerCfg, k: torch.Tensor, v: torch.Tensor, cache: QCache,
+                     dst_row: Optional[torch.Tensor] = None) -> None:
+    m, dt = k.shape[0], cfg.torch_dtype
+    if k.shape != (m, cfg.n_kv_heads, cfg.head_dim) or v.shape != k.shape:
+        raise ValueError("k/v must be [m, Hkv, D]")
+    if dst_row is not None and dst_row.shape != (m,):
+        raise ValueError("dst_row must be [m]")
+    own = _of_cache(cfg, cache)
+    ptrs = (_ptr(k, dt, "k"), _ptr(v, dt, "v"), _ptr(dst_row, torch.int32, "dst_row"))
+    _current(k, v, dst_row, own)
+    _check("pkv_qcache_store", load_library().pkv_qcache_store(
+        cfg._ref, *ptrs, cache._ref, m, _stream()))
+
+
+def pkv_qcache_restore(cfg: LayerCfg, cache: QCache, k_out: torch.Tensor, v_out: torch.Tensor,
+                       row_idx: Optional[torch.Tensor] = None,
+                       pos: Optional[torch.Tensor] = None, pos_base: int = 0,
+                       rotate: bool = True) -> None:
+    m, dt = k_out.shape[0], cfg.torch_dtype
+    if k_out.shape != (m, cfg.n_kv_heads, cfg.head_dim) or v_out.shape != k_out.shape:
+        raise ValueError("k_out/v_out must be [m, Hkv, D]")
+    for t, name in ((row_idx, "row_idx"), (pos, "pos")):
+        if t is not None and t.shape != (m,):
+            raise ValueError(f"{name} must be [m]")
+    own = _of_cache(cfg, cache)
+    ptrs = (_ptr(row_idx, torch.int32, "row_idx"), _ptr(pos, torch.int32, "pos"))
+    outs = (_ptr(k_out, dt, "k_out"), _ptr(v_out, dt, "v_out"))
+    _current(k_out, v_out, row_idx, pos, own)
+    _check("pkv_qcache_restore", load_library().pkv_qcache_restore(
+        cfg._ref, cache._ref, *ptrs, int(pos_base), int(bool(rotate)), *outs, m, _stream()))
+
+
+def pkv_qcache_attn_workspace_bytes(cfg: LayerCfg, rows: int, m: int, n_seq: int = 1) -> int:
+    return int(load_library().pkv_qcache_attn_workspace_bytes(cfg._ref, int(rows), int(m),
+                                                              int(n_seq)))
+
+
+def pkv_qcache_attn(cfg: LayerCfg, q: torch.Tensor, cache: QCache, row_pos: torch.Tensor,
+                    out: torch.Tensor, seq_start: Optional[torch.Tensor] = None, n_seq: int = 1,
+                    lse_out: Optional[torch.Tensor] = None, softmax_scale: float = 0.0,
+                    ws: Optional[torch.Tensor] = None) -> None:
+    m, dt = row_pos.shape[0], cfg.torch_dtype
+    if row_pos.dim() != 1 or q.shape != (m, cfg.n_q_heads, cfg.head_dim) or out.shape != q.shape:
+        raise ValueError("q/out must be [m, Hq, D], row_pos [m]")
+    if seq_start is not None and seq_start.shape != (n_seq,):
+        raise ValueError("seq_start must be [n_seq]")
+    if lse_out is not None and lse_out.shape != (m, cfg.n_q_heads):
+        raise ValueError("lse_out must be [m, Hq]")
+    own = _of_cache(cfg, cache)
+    qp = _ptr(q, dt, "q")
+    ptrs = (_ptr(row_pos, torch.int32, "row_pos"), _ptr(seq_start, torch.int32, "seq_start"),
+            _ptr(out, dt, "out"), _ptr(lse_out, torch.float32, "lse_out"))
+    wp, wb = _ws(ws)
+    _current(q, row_pos, seq_start, out, lse_out, ws, own)
+    _check("pkv_qcache_attn", load_library().pkv_qcache_attn(
+        cfg._ref, qp, cache._ref, *ptrs, m, int(n_seq), float(softmax_scale), wp, wb, _stream()))
 
 
 # ---- layer glue -------------------------------------------------------------------

@@ -23,7 +23,8 @@ SOURCES = ["pkv_api.hip", "rope_restore.hip", "query_score.hip", "query_score_dm
            "gather_qkv_proj_tiles.hip", "scatter_kv.hip", "layer_glue.hip",
            "static_scratch.hip", "f32_kernels.hip",
            "sparse_row_attn.hip", "sparse_row_attn_dma.hip", "sparse_row_attn_w8.hip",
-           "sparse_row_attn_w8n.hip", "sparse_row_attn_pair.hip", "sparse_row_attn_short.hip"]
+           "sparse_row_attn_w8n.hip", "sparse_row_attn_pair.hip", "sparse_row_attn_short.hip",
+           "packed_attn.hip", "qcache.hip", "qcache_attn.hip"]
 
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

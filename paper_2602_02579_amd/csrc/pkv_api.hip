@@ -32,6 +32,20 @@ float resolve_scale(float s, int head_dim) {
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
+template <typename... P>
+bool all_aligned16(P... ptrs) {
+    return ((reinterpret_cast<uintptr_t>(ptrs) | ...) & 15) == 0;
+}
+
+pkv_status check_qcache(const pkv_qcache* c) {
+    if (!c) return PKV_ERR_NULL;
+    if (c->rows <= 0 || c->rows > kMaxTokens || c->rows % 32) return PKV_ERR_SHAPE;
+    if (!c->k_codes || !c->k_scales || !c->v_codes || !c->v_scales) return PKV_ERR_NULL;
+    if (!all_aligned16(c->k_codes, c->k_scales, c->v_codes, c->v_scales))
+        return PKV_ERR_UNSUPPORTED;
+    return PKV_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -246,6 +260,89 @@ size_t pkv_chunk_attn_workspace_bytes(const pkv_layer_cfg* cfg, int64_t m, int64
         chunk_len > kMaxTokens)
         return 0;
     return align256(chunk_attn_ws_bytes(*cfg, m, chunk_len));
+}
+
+pkv_status pkv_packed_attn(const pkv_layer_cfg* cfg, const void* q, const void* k, const void* v,
+                           const int32_t* row_pos, void* out, float* lse_out, int64_t m,
+                           float softmax_scale, void* ws, size_t ws_bytes, void* stream) {
+    pkv_status st = check_cfg(cfg);
+    if (st != PKV_OK) return st;
+    if (m < 0 || m > kMaxTokens) return PKV_ERR_SHAPE;
+    if (!std::isfinite(softmax_scale) || softmax_scale < 0.f) return PKV_ERR_SHAPE;
+    if (m * (int64_t)cfg->n_q_heads > INT32_MAX) return PKV_ERR_UNSUPPORTED;
+    if (m == 0) return PKV_OK;
+    if (!q || !k || !v || !row_pos || !out) return PKV_ERR_NULL;
+    if (!all_aligned16(q, k, v, out)) return PKV_ERR_UNSUPPORTED;
+    const size_t need = align256(packed_attn_ws_bytes(*cfg, m));
+    if (need && (!ws || ws_bytes < need)) return PKV_ERR_WORKSPACE;
+    return launch_packed_attn(*cfg, q, k, v, row_pos, out, lse_out, m,
+                              resolve_scale(softmax_scale, cfg->head_dim), ws,
+                              (hipStream_t)stream);
+}
+
+size_t pkv_packed_attn_workspace_bytes(const pkv_layer_cfg* cfg, int64_t m) {
+    if (check_cfg(cfg) != PKV_OK || m <= 0 || m > kMaxTokens ||
+        m * (int64_t)cfg->n_q_heads > INT32_MAX)
+        return 0;
+    return align256(packed_attn_ws_bytes(*cfg, m));
+}
+
+pkv_status pkv_qcache_store(const pkv_layer_cfg* cfg, const void* k, const void* v,
+                            const int32_t* dst_row, const pkv_qcache* cache, int64_t m,
+                            void* stream) {
+    pkv_status st = check_cfg(cfg);
+    if (st != PKV_OK) return st;
+    if (m < 0 || m > kMaxTokens) return PKV_ERR_SHAPE;
+    if ((st = check_qcache(cache)) != PKV_OK) return st;
+    if (!dst_row && m > cache->rows) return PKV_ERR_SHAPE;
+    if (m == 0) return PKV_OK;
+    if (!k || !v) return PKV_ERR_NULL;
+    if (!all_aligned16(k, v)) return PKV_ERR_UNSUPPORTED;
+    return launch_qcache_store(*cfg, k, v, dst_row, *cache, m, (hipStream_t)stream);
+}
+
+pkv_status pkv_qcache_restore(const pkv_layer_cfg* cfg, const pkv_qcache* cache,
+                              const int32_t* row_idx, const int32_t* pos, int64_t pos_base,
+                              int rotate, void* k_out, void* v_out, int64_t m, void* stream) {
+    pkv_status st = check_cfg(cfg);
+    if (st != PKV_OK) return st;
+    if (m < 0 || m > kMaxTokens) return PKV_ERR_SHAPE;
+    if ((st = check_qcache(cache)) != PKV_OK) return st;
+    if (!row_idx && m > cache->rows) return PKV_ERR_SHAPE;
+    if (!pos && (pos_base < -kMaxTokens || pos_base > kMaxTokens)) return PKV_ERR_SHAPE;
+    if (m == 0) return PKV_OK;
+    if (!k_out || !v_out) return PKV_ERR_NULL;
+    if (!all_aligned16(k_out, v_out)) return PKV_ERR_UNSUPPORTED;
+    return launch_qcache_restore(*cfg, *cache, row_idx, pos, pos_base, rotate != 0, k_out, v_out,
+                                 m, (hipStream_t)stream);
+}
+
+pkv_status pkv_qcache_attn(const pkv_layer_cfg* cfg, const void* q, const pkv_qcache* cache,
+                           const int32_t* row_pos, const int32_t* seq_start, void* out,
+                           float* lse_out, int64_t m, int64_t n_seq, float softmax_scale,
+                           void* ws, size_t ws_bytes, void* stream) {
+    pkv_status st = check_cfg(cfg);
+    if (st != PKV_OK) return st;
+    if (m < 0 || m > kMaxTokens || n_seq <= 0 || m % n_seq) return PKV_ERR_SHAPE;
+    if (!std::isfinite(softmax_scale) || softmax_scale < 0.f) return PKV_ERR_SHAPE;
+    if ((st = check_qcache(cache)) != PKV_OK) return st;
+    if (m * (int64_t)cfg->n_q_heads > INT32_MAX) return PKV_ERR_UNSUPPORTED;
+    if (m == 0) return PKV_OK;
+    if (!q || !row_pos || !out) return PKV_ERR_NULL;
+    if (!all_aligned16(q, out)) return PKV_ERR_UNSUPPORTED;
+    const size_t need = align256(qcache_attn_ws_bytes(*cfg, cache->rows, m, n_seq));
+    if (need && (!ws || ws_bytes < need)) return PKV_ERR_WORKSPACE;
+    return launch_qcache_attn(*cfg, q, *cache, row_pos, seq_start, out, lse_out, m, n_seq,
+                              resolve_scale(softmax_scale, cfg->head_dim), ws,
+                              (hipStream_t)stream);
+}
+
+size_t pkv_qcache_attn_workspace_bytes(const pkv_layer_cfg* cfg, int64_t rows, int64_t m,
+                                       int64_t n_seq) {
+    if (check_cfg(cfg) != PKV_OK || rows <= 0 || rows > kMaxTokens || rows % 32 || m <= 0 ||
+        m > kMaxTokens || n_seq <= 0 || m % n_seq || m * (int64_t)cfg->n_q_heads > INT32_MAX)
+        return 0;
+    return align256(qcache_attn_ws_bytes(*cfg, rows, m, n_seq));
 }
 
 pkv_status pkv_sparse_row_attn_ctx_lse(const pkv_layer_cfg* cfg, const void* q,

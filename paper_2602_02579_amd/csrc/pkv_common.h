@@ -139,6 +139,25 @@ pkv_status launch_chunk_attn(const pkv_layer_cfg& cfg, const void* q, const void
                              const void* v, const int32_t* row_pos, void* out, int64_t m,
                              int64_t chunk_len, float scale, void* ws, hipStream_t st);
 
+// packed_attn.hip
+size_t packed_attn_ws_bytes(const pkv_layer_cfg& cfg, int64_t m);
+pkv_status launch_packed_attn(const pkv_layer_cfg& cfg, const void* q, const void* k,
+                              const void* v, const int32_t* row_pos, void* out, float* lse_out,
+                              int64_t m, float scale, void* ws, hipStream_t st);
+
+// qcache.hip, qcache_attn.hip
+pkv_status launch_qcache_store(const pkv_layer_cfg& cfg, const void* k, const void* v,
+                               const int32_t* dst_row, const pkv_qcache& cache, int64_t m,
+                               hipStream_t st);
+pkv_status launch_qcache_restore(const pkv_layer_cfg& cfg, const pkv_qcache& cache,
+                                 const int32_t* row_idx, const int32_t* pos, int64_t pos_base,
+                                 bool rotate, void* k_out, void* v_out, int64_t m, hipStream_t st);
+size_t qcache_attn_ws_bytes(const pkv_layer_cfg& cfg, int64_t rows, int64_t m, int64_t n_seq);
+pkv_status launch_qcache_attn(const pkv_layer_cfg& cfg, const void* q, const pkv_qcache& cache,
+                              const int32_t* row_pos, const int32_t* seq_start, void* out,
+                              float* lse_out, int64_t m, int64_t n_seq, float scale, void* ws,
+                              hipStream_t st);
+
 // layer glue (layer_glue.hip); dtype is a pkv_dtype
 pkv_status launch_rmsnorm_rows(int dtype, const void* h, const int32_t* row_idx,
                                const void* weight, float eps, void* y, int64_t m,
