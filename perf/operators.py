@@ -305,7 +305,8 @@ def run(s):
             return s["out"], s["lse"]
         if s["kind"] == "keep":
             api.pkv_qcache_store(s["cfg"], s["k"], s["v"], s["cache"])
-        api.pkv_qcache_restore(s["cfg"], s["cache"], s["k_out"], s["v_out"], s.get("rows"), s["pos"])
+        api.pkv_qcache_restore(s["cfg"], s["cache"], s["k_out"], s["v_out"],
+                               s["rows"] if s["kind"] == "fetch" else None, s["pos"])
         return s["k_out"], s["v_out"]
 
     hq, hkv, d = s["heads"]
