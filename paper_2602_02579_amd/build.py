@@ -41,6 +41,7 @@ SOURCE_FLAGS = {
     "sparse_row_attn_pair.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "sparse_row_attn_short.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "query_score_dma.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+    "packed_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "qcache_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "gather_qkv_proj_tiles.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
 }

@@ -1,31 +1,549 @@
 // Causal attention over a packed prompt: row i attends the row_pos[i] + 1 rows that end with itself.
 // (Paper: Sec. 2 - the method's input are chunks that were prefilled one by one.)
-#include "attn_rows_simple.h"
+//
+// bf16: S^T = K Q^T,  O^T += V^T P^T  (v_mfma_f32_32x32x16_bf16), softmax along a lane's registers.
+// A workgroup of four waves owns 128 consecutive (row, head of the group) columns of a kv head, 32 a
+// wave, whichever sequences they belong to: many short sequences fill a tile as well as a long
+// one, and the tiles are known without a look at the lengths.  It goes over the keys from the first
+// that one of its rows sees to the last, 64 at a time; every column masks with its own two ends, and
+// a wave skips what none of its columns sees.  K and V tiles come into LDS by direct loads, the
+// next one while one is used; 64 KB (head_dim 128) leave room for a second workgroup on the CU, whose
+// products run under this one's exponentials.
+//
+// The reference of a column's exponentials follows the running maximum only when that is 2^8 or more
+// above it: most tiles neither rescale nor exchange anything between lanes.
+#include <atomic>
+
+#include "attn_common.h"
+#include "attn_tile.h"
 
 namespace pkv {
 
 namespace {
 
 template <typename T>
-struct RowsOfPrompt {
-    const T *k, *v;   // of the kv head
-    int64_t stride;
-    __device__ float key(int64_t t, int d) const { return Elem<T>::load(k + t * stride + d); }
-    __device__ float value(int64_t t, int d) const { return Elem<T>::load(v + t * stride + d); }
+struct PackedParams {
+    const T *q, *k, *v;
+    const int32_t* row_pos;
+    T* out;
+    float* lse;
+    int m, hq, hkv, group, D, n_tiles;
+    float c2;   // softmax scale * log2(e)
 };
 
+constexpr float kLn2 = 0.69314718055994531f;
+constexpr int kCols = 128;     // columns of a workgroup, bf16
+constexpr int kThreads = 256;
+
+// What a row sees: keys lo <= t < hi (nothing: hi == 0)
+__device__ __forceinline__ void keys_of(const int32_t* row_pos, int row, bool valid, int* lo,
+                                        int* hi) {
+    *lo = 0x7fffffff;
+    *hi = 0;
+    if (!valid) return;
+    const int pos = min(row_pos[row], row);
+    if (pos < 0) return;
+    *lo = row - pos;
+    *hi = row + 1;
+}
+
+// One (row, head) by a wave, key by key, nothing but the keys that it sees: for columns whose result is
+// not finite.  A value that is not finite in a key of the tile that the column does not see comes
+// into the products above as 0 times infinity; here it does not.
+template <typename T, int DP>
+__device__ void attend_alone(const PackedParams<T>& p, int row, int h, int g, int lo, int hi) {
+    constexpr int E = DP / 64;
+    const int lane = threadIdx.x & 63;
+    const int64_t o = ((int64_t)row * p.hq + h) * p.D;
+    float q[E], acc[E], mx = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        q[e] = lane + 64 * e < p.D ? Elem<T>::load(p.q + o + lane + 64 * e) : 0.f;
+        acc[e] = 0.f;
+    }
+    for (int t = lo; t < hi; ++t) {
+        const int64_t at = ((int64_t)t * p.hkv + g) * p.D;
+        float s = 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (lane + 64 * e < p.D) s += q[e] * Elem<T>::load(p.k + at + lane + 64 * e);
+#pragma unroll
+        for (int x = 32; x > 0; x >>= 1) s += __shfl_xor(s, x);
+        s *= p.c2;
+        const float m = fmaxf(mx, s), ref = m == -INFINITY ? 0.f : m;
+        const float corr = __builtin_amdgcn_exp2f(mx - ref), w = __builtin_amdgcn_exp2f(s - ref);
+        mx = m;
+        sum = sum * corr + w;
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (lane + 64 * e < p.D) acc[e] = acc[e] * corr + w * Elem<T>::load(p.v + at + lane + 64 * e);
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+        if (lane + 64 * e < p.D) p.out[o + lane + 64 * e] = Elem<T>::from_f32(acc[e] / sum);
+    if (lane == 0 && p.lse)
+        p.lse[(int64_t)row * p.hq + h] = (mx + __builtin_amdgcn_logf(sum)) * kLn2;
+}
+
+// DP: head_dim rounded up to 64, 128 or 256.  Elements between are 0 in the queries; in the tiles they
+// repeat others of the same row.
+template <int DP>
+__global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void packed_attn_kernel(PackedParams<bf16_t> p) {
+    constexpr int KC = DP / 16;               // contraction steps of a score
+    constexpr int DB = DP / 32;               // 32-row blocks of O^T
+    constexpr int CH = DP / 8;                // 16-byte pieces of a row
+    constexpr int kRow = DP * 2;              // bytes of a row in LDS
+    constexpr int kTile = kBN * kRow;         // 64 keys of K or of V
+    constexpr int FILLS = kTile / 1024 / 4;   // instructions of a wave for a tile
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ int s_lo[4], s_hi[4];
+
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int hh = lane >> 5, l32 = lane & 31;
+    const int g = blockIdx.x % p.hkv;
+    const int tile = p.n_tiles - 1 - (int)(blockIdx.x / p.hkv);   // later rows see more: first
+
+    // ---- this lane's column ---------------------------------------------------------------------
+    const int64_t col = (int64_t)tile * kCols + wave * 32 + l32;
+    const int row = (int)(col / p.group), head = g * p.group + (int)(col - (int64_t)row * p.group);
+    const bool valid = row < p.m;
+    int lo, hi;
+    keys_of(p.row_pos, row, valid, &lo, &hi);
+    bf16x8 qreg[KC];
+    {
+        const bf16_t* qp = p.q + ((int64_t)row * p.hq + head) * p.D + hh * 8;
+#pragma unroll
+        for (int kc = 0; kc < KC; ++kc) {
+            bf16x8 z = {};
+            if (valid && kc * 16 + hh * 8 < p.D) z = *reinterpret_cast<const bf16x8*>(qp + kc * 16);
+            qreg[kc] = z;
+        }
+    }
+    // what some column of the wave sees, and what all of them that see anything do
+    int w_lo = lo, w_hi = hi, in_lo = hi ? lo : 0, in_hi = hi ? hi : 0x7fffffff;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        w_lo = min(w_lo, __shfl_xor(w_lo, o));
+        w_hi = max(w_hi, __shfl_xor(w_hi, o));
+        in_lo = max(in_lo, __shfl_xor(in_lo, o));
+        in_hi = min(in_hi, __shfl_xor(in_hi, o));
+    }
+    w_lo = __builtin_amdgcn_readfirstlane(w_lo);
+    w_hi = __builtin_amdgcn_readfirstlane(w_hi);
+    in_lo = __builtin_amdgcn_readfirstlane(in_lo);
+    in_hi = __builtin_amdgcn_readfirstlane(in_hi);
+    if (lane == 0) {
+        s_lo[wave] = w_lo;
+        s_hi[wave] = w_hi;
+    }
+    __syncthreads();
+    const int k_lo = __builtin_amdgcn_readfirstlane(min(min(s_lo[0], s_lo[1]), min(s_lo[2], s_lo[3])));
+    const int k_hi = __builtin_amdgcn_readfirstlane(max(max(s_hi[0], s_hi[1]), max(s_hi[2], s_hi[3])));
+    const int n_iter = k_hi > k_lo ? (k_hi - k_lo + kBN - 1) / kBN : 0;
+
+    // ---- global -> LDS -----------------------------------------------------------------------------
+    // Piece c of K row r lies at c ^ swizzle: the rows of one operand read are in different banks.  V
+    // likewise, for the four rows of a transposing read.
+    auto k_swz = [](int r) { return DP == 64 ? (r >> 1) & 7 : r & 15; };
+    auto v_swz = [](int r) { return DP == 64 ? 2 * (r & 2) : 4 * (r & 3); };
+    const uint32_t lds = (uint32_t)(uintptr_t)smem;
+    const uint32_t lds_fill = __builtin_amdgcn_readfirstlane(lds + wave * FILLS * 1024);
+    const uint32_t row_bytes = (uint32_t)p.hkv * p.D * 2;
+    const int last_piece = p.D / 8 - 1;
+    uint32_t k_off[FILLS], v_off[FILLS];
+#pragma unroll
+    for (int i = 0; i < FILLS; ++i) {
+        const int x = (wave * FILLS + i) * 64 + lane, r = x / CH, c = x % CH;
+        k_off[i] = (uint32_t)min(c ^ k_swz(r), last_piece) * 16;
+        v_off[i] = (uint32_t)min(c ^ v_swz(r), last_piece) * 16;
+    }
+    const bf16_t* const k_head = p.k + ((int64_t)k_lo * p.hkv + g) * p.D;
+    const bf16_t* const v_head = p.v + ((int64_t)k_lo * p.hkv + g) * p.D;
+    auto fill = [&](int t) {
+        const int last = k_hi - k_lo - 1 - t * kBN;    // rows behind the last one repeat it
+        const int64_t base = (int64_t)t * kBN * p.hkv * p.D;
+        const uint32_t dst = lds_fill + (t & 1) * 2 * kTile;
+#pragma unroll
+        for (int i = 0; i < FILLS; ++i) {
+            const int r = min(((wave * FILLS + i) * 64 + lane) / CH, last);
+            dma16(k_head + base, (uint32_t)r * row_bytes + k_off[i], dst + i * 1024);
+            dma16(v_head + base, (uint32_t)r * row_bytes + v_off[i], dst + kTile + i * 1024);
+        }
+    };
+
+    // ---- LDS -> operands -----------------------------------------------------------------------------
+    // A row i of a 32-key block is key swap_bits_2_3(i): a lane's 16 scores are then the keys 8 hh + 0..7
+    // and 16 + 8 hh + 0..7, the B operands of the second product
+    const int prow = (l32 & 0x13) | ((l32 & 4) << 1) | ((l32 & 8) >> 1);
+    uint32_t kaddr[KC], vaddr[DB];
+#pragma unroll
+    for (int kc = 0; kc < KC; ++kc)
+        kaddr[kc] = (uint32_t)(prow * kRow + (((2 * kc + hh) ^ k_swz(prow)) * 16));
+    {
+        const int e = (lane >> 2) & 3, j = lane & 3, gh = (lane >> 4) & 1;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+            vaddr[db] = (uint32_t)(kTile + (8 * hh + e) * kRow +
+                                   ((db * 4 + gh * 2 + (j >> 1)) ^ v_swz(e)) * 16 + (j & 1) * 8);
+    }
+
+    float m2 = -INFINITY, l_run = 0.f;     // l_run: this lane's keys only
+    f32x16 o_acc[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o_acc[db][r] = 0.f;
+
+    if (n_iter > 0) fill(0);
+    if (n_iter > 1) fill(1);
+    for (int t = 0; t < n_iter; ++t) {
+        if (t + 1 < n_iter) wait_vm<2 * FILLS>();   // this tile has landed, the next is on its way
+        else wait_vm<0>();
+        __syncthreads();
+        const int key0 = k_lo + t * kBN;
+        if (key0 < w_hi && key0 + kBN > w_lo) {
+            const unsigned char* st = smem + (t & 1) * 2 * kTile;
+            f32x16 s[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[h][r] = 0.f;
+#pragma unroll
+            for (int kc = 0; kc < KC; ++kc)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    s[h] = mfma32(*reinterpret_cast<const bf16x8*>(st + h * 32 * kRow + kaddr[kc]),
+                                  qreg[kc], s[h]);
+            if (key0 < in_lo || key0 + kBN > in_hi) {
+                // element r of block h is key 32 h + 16 (r / 8) + 8 hh + r % 8 of the tile
+                const int a = lo - key0 - 8 * hh, b = hi - key0 - 8 * hh;
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int key = 32 * h + 16 * (r / 8) + r % 8;
+                        if (key < a || key >= b) s[h][r] = -INFINITY;
+                    }
+            }
+            float top = s[0][0];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) top = fmaxf(top, s[h][r]);
+            top *= p.c2;
+            if (__any(top > m2 + 8.f)) {
+                float mx = fmaxf(top, m2);
+                mx = fmaxf(mx, __shfl_xor(mx, 32));
+                const float corr = mx == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m2 - mx);
+                m2 = mx;
+                l_run *= corr;
+#pragma unroll
+                for (int db = 0; db < DB; ++db)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) o_acc[db][r] *= corr;
+            }
+            const float ref = m2 == -INFINITY ? 0.f : m2;
+            bf16x8 pb[2][2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const float e = __builtin_amdgcn_exp2f(fmaf(s[h][r], p.c2, -ref));
+                    l_run += e;
+                    pb[h][r / 8][r % 8] = (bf16_t)e;
+                }
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+                    for (int db = 0; db < DB; ++db) {
+                        const unsigned char* a = st + (32 * h + 16 * kk) * kRow + vaddr[db];
+                        const bf16x4 x = lds_read_tr(a), y = lds_read_tr(a + 4 * kRow);
+                        const bf16x8 va = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+                        o_acc[db] = mfma32(va, pb[h][kk], o_acc[db]);
+                    }
+        }
+        __syncthreads();                            // everybody is done with this tile
+        if (t + 2 < n_iter) fill(t + 2);
+    }
+
+    // ---- results -----------------------------------------------------------------------------------
+    const float l = l_run + __shfl_xor(l_run, 32);
+    const float inv = hi ? 1.f / l : 0.f;
+    bool fine = true;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            o_acc[db][r] = hi ? o_acc[db][r] * inv : 0.f;
+            fine = fine && fabsf(o_acc[db][r]) < INFINITY;
+        }
+    fine = fine && (hi == 0 || l < INFINITY);
+    const uint64_t not_fine = __ballot(!fine && valid);
+    const uint32_t alone = (uint32_t)(not_fine | not_fine >> 32);   // by column
+    if (valid && !(alone >> l32 & 1)) {
+        const int64_t oc = (int64_t)row * p.hq + head;
+        bf16_t* op = p.out + oc * p.D + 4 * hh;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int r4 = 0; r4 < 4; ++r4) {
+                bf16x4 x;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = (bf16_t)o_acc[db][4 * r4 + e];
+                if (db * 32 + r4 * 8 + 4 * hh < p.D)
+                    *reinterpret_cast<bf16x4*>(op + db * 32 + r4 * 8) = x;
+            }
+        if (hh == 0 && p.lse)
+            p.lse[oc] = hi ? (m2 + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+    }
+    for (uint32_t left = alone; left; left &= left - 1) {
+        const int at = __builtin_ctz(left);
+        attend_alone<bf16_t, DP>(p, __shfl(row, at), __shfl(head, at), g, __shfl(lo, at), __shfl(hi, at));
+    }
+}
+
+// ---- fp32 ----------------------------------------------------------------------------------------
+// v_mfma_f32_16x16x4_f32: a workgroup owns 16 columns of a kv head, its NW waves take every NW-th tile of
+// 16 keys and meet in LDS.  Operands come from global memory as they lie there: lane group g4 of a
+// contraction takes elements 4 g4 .. + 3 of every 16, a lane's scores (keys 4 g4 + r) are the B
+// operand of the second product, and row i of output block c is element C i + c of the head, so that
+// a lane's piece of a value row is C consecutive floats.  The next tile is requested before the current
+// one is used.  WIDE: head_dim is DP.
+__device__ __forceinline__ f32x4 mfma_f32(float a, float b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
+}
+
+template <int DP, int NW, bool WIDE>
+__global__ __launch_bounds__(NW * 64) void packed_attn_f32_kernel(PackedParams<float> p) {
+    constexpr int CM = DP / 16, kColRow = 17;       // 17: the join reads down the columns
+    extern __shared__ __align__(16) float s_part[];   // [NW][DP][17]
+    __shared__ float s_m[NW][16], s_l[NW][16];
+    __shared__ int s_col[16][4];                    // row, head, lo, hi
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int g4 = lane >> 4, l16 = lane & 15;
+    const int g = blockIdx.y, D = WIDE ? DP : p.D, C = D / 16;
+    const int64_t col = (int64_t)(gridDim.x - 1 - blockIdx.x) * 16 + l16;   // later rows first
+    const int row = (int)(col / p.group), head = g * p.group + (int)(col - (int64_t)row * p.group);
+    const bool valid = row < p.m;
+    int lo, hi;
+    keys_of(p.row_pos, row, valid, &lo, &hi);
+    int k_lo = lo, k_hi = hi;
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) {
+        k_lo = min(k_lo, __shfl_xor(k_lo, o));
+        k_hi = max(k_hi, __shfl_xor(k_hi, o));
+    }
+    k_lo = __builtin_amdgcn_readfirstlane(k_lo);
+    k_hi = __builtin_amdgcn_readfirstlane(k_hi);
+
+    const int64_t krow = (int64_t)p.hkv * D;
+    const float* const kb = p.k + (int64_t)g * D + 4 * g4;
+    const float* const vb = p.v + (int64_t)g * D + C * l16;
+    f32x4 q4[CM], k4[CM], kn[CM], o_acc[CM];
+    float v4[4][CM], vn[4][CM];
+    {
+        const float* const qp = p.q + ((int64_t)(valid ? row : 0) * p.hq + head) * D + 4 * g4;
+#pragma unroll
+        for (int c = 0; c < CM; ++c) {
+            o_acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+            q4[c] = o_acc[c];
+            if (valid && (WIDE || c < C)) q4[c] = *reinterpret_cast<const f32x4*>(qp + 16 * c);
+        }
+    }
+    auto load = [&](int t0) {                       // keys behind the last one repeat it
+        const float* const k = kb + min(t0 + l16, k_hi - 1) * krow;
+#pragma unroll
+        for (int c = 0; c < CM; ++c)
+            if (WIDE || c < C) kn[c] = *reinterpret_cast<const f32x4*>(k + 16 * c);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float* const v = vb + min(t0 + 4 * g4 + j, k_hi - 1) * krow;
+            if constexpr (WIDE) {
+#pragma unroll
+                for (int c = 0; c < CM; c += 4) {
+                    const f32x4 x = *reinterpret_cast<const f32x4*>(v + c);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) vn[j][c + i] = x[i];
+                }
+            } else {
+#pragma unroll
+                for (int c = 0; c < CM; ++c)
+                    if (c < C) vn[j][c] = v[c];
+            }
+        }
+    };
+    float m2 = -INFINITY, sum = 0.f;                // sum: this lane group's keys only
+    int t0 = k_lo + wave * 16;                      // (nothing to see: k_lo is the largest number)
+    bool more = k_hi > 0 && t0 < k_hi;
+    if (more) load(t0);
+    while (more) {
+#pragma unroll
+        for (int c = 0; c < CM; ++c) k4[c] = kn[c];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int c = 0; c < CM; ++c) v4[j][c] = vn[j][c];
+        const int t = t0;
+        t0 += NW * 16;
+        more = t0 < k_hi;
+        if (more) load(t0);
+        f32x4 s = {0.f, 0.f, 0.f, 0.f}, s2 = s;     // two chains: half the latency
+#pragma unroll
+        for (int c = 0; c < CM; ++c)
+            if (WIDE || c < C)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (c & 1) s2 = mfma_f32(k4[c][j], q4[c][j], s2);
+                    else s = mfma_f32(k4[c][j], q4[c][j], s);
+                }
+        s += s2;
+        float top = -INFINITY;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int key = t + 4 * g4 + r;
+            s[r] = key >= lo && key < hi ? s[r] * p.c2 : -INFINITY;
+            top = fmaxf(top, s[r]);
+        }
+        if (__any(top > m2 + 8.f)) {
+            float m = fmaxf(top, m2);
+            m = fmaxf(m, __shfl_xor(m, 16));
+            m = fmaxf(m, __shfl_xor(m, 32));
+            const float corr = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m2 - m);
+            m2 = m;
+            sum *= corr;
+#pragma unroll
+            for (int c = 0; c < CM; ++c) o_acc[c] *= corr;
+        }
+        const float ref = m2 == -INFINITY ? 0.f : m2;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            s[r] = __builtin_amdgcn_exp2f(s[r] - ref);
+            sum += s[r];
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int c = 0; c < CM; ++c)
+                if (WIDE || c < C) o_acc[c] = mfma_f32(v4[j][c], s[j], o_acc[c]);
+    }
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    if (g4 == 0) {
+        s_m[wave][l16] = m2;
+        s_l[wave][l16] = sum;
+        if (wave == 0) {
+            s_col[l16][0] = valid ? row : -1;
+            s_col[l16][1] = head;
+            s_col[l16][2] = lo;
+            s_col[l16][3] = hi;
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < CM; ++c)
+        if (WIDE || c < C)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                s_part[(wave * DP + C * (4 * g4 + r) + c) * kColRow + l16] = o_acc[c][r];
+    __syncthreads();
+    // a column's elements are written by one wave, so that a row of queries that its result replaces is
+    // still there where the column has to be attended alone
+    for (int cc = wave; cc < 16; cc += NW) {
+        const int r = s_col[cc][0], h = s_col[cc][1];
+        if (r < 0) continue;
+        float top = -INFINITY, l = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) top = fmaxf(top, s_m[w][cc]);
+        const float ref = top == -INFINITY ? 0.f : top;
+        float f[NW];
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            f[w] = __builtin_amdgcn_exp2f(s_m[w][cc] - ref);
+            l += s_l[w][cc] * f[w];
+        }
+        const bool sees = s_col[cc][3] > 0;
+        const float inv = sees ? 1.f / l : 0.f;
+        const int64_t oc = (int64_t)r * p.hq + h;
+        float x[DP / 64];
+        bool fine = !sees || l < INFINITY;
+#pragma unroll
+        for (int i = 0; i < DP / 64; ++i) {
+            const int d = lane + 64 * i;
+            x[i] = 0.f;
+            if (d < D && sees) {
+#pragma unroll
+                for (int w = 0; w < NW; ++w) x[i] += s_part[(w * DP + d) * kColRow + cc] * f[w];
+                x[i] *= inv;
+                fine = fine && fabsf(x[i]) < INFINITY;
+            }
+        }
+        if (__any(!fine)) {
+            attend_alone<float, DP>(p, r, h, g, s_col[cc][2], s_col[cc][3]);
+            continue;
+        }
+#pragma unroll
+        for (int i = 0; i < DP / 64; ++i)
+            if (lane + 64 * i < D) p.out[oc * D + lane + 64 * i] = x[i];
+        if (lane == 0 && p.lse)
+            p.lse[oc] = sees ? (top + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+    }
+}
+
 template <typename T>
-__global__ __launch_bounds__(64) void packed_simple_kernel(const T* q, const T* k, const T* v,
-                                                           const int32_t* row_pos, T* out,
-                                                           float* lse, int hq, int hkv, int D,
-                                                           float scale) {
-    const int64_t row = blockIdx.x / hq;
-    const int h = blockIdx.x % hq, g = h / (hq / hkv);
-    const int64_t pos = row_pos[row] < row ? row_pos[row] : row;
-    const RowsOfPrompt<T> src = {k + g * D, v + g * D, (int64_t)hkv * D};
-    const int64_t o = row * hq + h;
-    attend_simple<T>(q + o * D, src, pos < 0 ? row + 1 : row - pos, row + 1, D, scale, out + o * D,
-                     lse ? lse + o : nullptr);
+PackedParams<T> params(const pkv_layer_cfg& cfg, const void* q, const void* k, const void* v,
+                       const int32_t* row_pos, void* out, float* lse, int64_t m, float scale) {
+    PackedParams<T> p = {};
+    p.q = static_cast<const T*>(q);
+    p.k = static_cast<const T*>(k);
+    p.v = static_cast<const T*>(v);
+    p.row_pos = row_pos;
+    p.out = static_cast<T*>(out);
+    p.lse = lse;
+    p.m = (int)m;
+    p.hq = cfg.n_q_heads;
+    p.hkv = cfg.n_kv_heads;
+    p.group = p.hq / p.hkv;
+    p.D = cfg.head_dim;
+    p.n_tiles = (int)ceil_div(m * p.group, kCols);
+    p.c2 = scale * 1.4426950408889634f;
+    return p;
+}
+
+// more LDS than a kernel gets unasked; set twice at worst, the calls are idempotent
+template <typename Kernel>
+bool allow_lds(Kernel kernel, int bytes, std::atomic<bool>* done) {
+    if (done->load(std::memory_order_acquire)) return true;
+    if (hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                            hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess)
+        return false;
+    done->store(true, std::memory_order_release);
+    return true;
+}
+
+template <int DP>
+pkv_status launch_tiles(const PackedParams<bf16_t>& p, hipStream_t st) {
+    constexpr int kBytes = 4 * kBN * DP * 2;
+    static std::atomic<bool> done{false};
+    if (!allow_lds(packed_attn_kernel<DP>, kBytes, &done)) return PKV_ERR_LAUNCH;
+    const int64_t grid = (int64_t)p.n_tiles * p.hkv;
+    if (grid >= (int64_t)1 << 24) return PKV_ERR_UNSUPPORTED;
+    hipLaunchKernelGGL(packed_attn_kernel<DP>, dim3((unsigned)grid), dim3(kThreads), kBytes, st, p);
+    return launch_status();
+}
+
+template <int DP, int NW, bool WIDE>
+pkv_status launch_f32(const PackedParams<float>& p, hipStream_t st) {
+    constexpr int kBytes = NW * DP * 17 * 4;
+    static std::atomic<bool> done{false};
+    if (!allow_lds(packed_attn_f32_kernel<DP, NW, WIDE>, kBytes, &done)) return PKV_ERR_LAUNCH;
+    const int64_t tiles = ceil_div((int64_t)p.m * p.group, 16);
+    if (tiles >= 1 << 22 || p.hkv > 65535) return PKV_ERR_UNSUPPORTED;
+    hipLaunchKernelGGL((packed_attn_f32_kernel<DP, NW, WIDE>), dim3((unsigned)tiles, (unsigned)p.hkv),
+                       dim3(NW * 64), kBytes, st, p);
+    return launch_status();
 }
 
 }  // namespace
@@ -35,16 +553,19 @@ size_t packed_attn_ws_bytes(const pkv_layer_cfg&, int64_t) { return 0; }
 pkv_status launch_packed_attn(const pkv_layer_cfg& cfg, const void* q, const void* k,
                               const void* v, const int32_t* row_pos, void* out, float* lse_out,
                               int64_t m, float scale, void*, hipStream_t st) {
-    const dim3 grid((unsigned)(m * cfg.n_q_heads));
-    if (cfg.dtype == PKV_BF16)
-        hipLaunchKernelGGL((packed_simple_kernel<bf16_t>), grid, dim3(64), 0, st, (const bf16_t*)q,
-                           (const bf16_t*)k, (const bf16_t*)v, row_pos, (bf16_t*)out, lse_out,
-                           cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim, scale);
-    else
-        hipLaunchKernelGGL((packed_simple_kernel<float>), grid, dim3(64), 0, st, (const float*)q,
-                           (const float*)k, (const float*)v, row_pos, (float*)out, lse_out,
-                           cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim, scale);
-    return launch_status();
+    const int d = cfg.head_dim;
+    if (cfg.dtype == PKV_BF16) {
+        const auto p = params<bf16_t>(cfg, q, k, v, row_pos, out, lse_out, m, scale);
+        return d <= 64 ? launch_tiles<64>(p, st)
+                       : d <= 128 ? launch_tiles<128>(p, st) : launch_tiles<256>(p, st);
+    }
+    const auto p = params<float>(cfg, q, k, v, row_pos, out, lse_out, m, scale);
+    // as many waves as their registers and parts leave room for
+    if (d == 64) return launch_f32<64, 16, true>(p, st);
+    if (d == 128) return launch_f32<128, 8, true>(p, st);
+    if (d == 256) return launch_f32<256, 4, true>(p, st);
+    if (d < 64) return launch_f32<64, 8, false>(p, st);
+    return d < 128 ? launch_f32<128, 4, false>(p, st) : launch_f32<256, 4, false>(p, st);
 }
 
 }  // namespace pkv
