@@ -4,7 +4,7 @@
 //
 // 16 columns (row, head of the group) share the keys of a kv head.  A wave takes 32 keys at a time,
 // straight from global memory into registers and from there, converted, into the matrix
-// instructions: both layouts are such that no lane needs what another one loaded.
+// instructions: both layouts are such that no lane needs what another one loaded (head_dim 128):
 //   Keys: lane (g4, l16) holds 32 consecutive elements of key 8 (l16 / 4) + l16 % 4 (+ 4 for the
 //     second half), 16 bytes; contraction index 8 g4 + e of step f is element 32 g4 + 8 f + e, on
 //     both sides.  Row 4 a + i of half kt being key 8 a + 4 kt + i, a lane ends with the scores of keys
@@ -26,6 +26,7 @@
 // whatever the lengths; a workgroup's piece may begin and end inside sequences.  What several
 // workgroups hold parts of goes to the workspace, and a second launch joins it.
 #include <algorithm>
+#include <atomic>
 
 #include "qcache.h"
 
@@ -36,9 +37,10 @@ namespace {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kWaves = 4;
+constexpr int kWaves = 8;
 constexpr int kGroup = kWaves * 32;   // keys of a workgroup's step
 constexpr int kJoinWaves = 8;
+constexpr float kLn2 = 0.69314718055994531f;
 
 struct QAttnParams {
     const void* q;                // [m, hq, D]
@@ -57,13 +59,32 @@ struct QAttnParams {
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
+// v of another lane of the 16 (a rotation), and of lanes in front (0 where there are none)
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ int dpp(int old, int v) {
+    return __builtin_amdgcn_update_dpp(old, v, CTRL, ROWS, 0xf, false);
+}
+__device__ __forceinline__ int min16(int v) {
+    v = min(v, dpp<0x128>(v, v));
+    v = min(v, dpp<0x124>(v, v));
+    v = min(v, dpp<0x122>(v, v));
+    return min(v, dpp<0x121>(v, v));
+}
+__device__ __forceinline__ int max16(int v) { return -min16(-v); }
+
 // The cache rows of a sequence from `start` on; row_end: the first one that a row does not see
+__device__ __forceinline__ int start_in_cache(const QAttnParams& p, int start) {
+    return min(max(start, 0), p.rows);
+}
 __device__ __forceinline__ int seq_start(const QAttnParams& p, int s) {
-    return p.seq_start ? min(max(p.seq_start[s], 0), p.rows) : 0;
+    return p.seq_start ? start_in_cache(p, p.seq_start[s]) : 0;
+}
+__device__ __forceinline__ int end_of(const QAttnParams& p, int start, int pos) {
+    const int64_t e = (int64_t)start + pos + 1;
+    return max(start, (int)min(e, (int64_t)p.rows));
 }
 __device__ __forceinline__ int row_end(const QAttnParams& p, int start, int row) {
-    const int64_t e = (int64_t)start + p.row_pos[row] + 1;
-    return max(start, (int)min(e, (int64_t)p.rows));
+    return end_of(p, start, p.row_pos[row]);
 }
 __device__ __forceinline__ int seq_end(const QAttnParams& p, int start, int s) {
     int end = start;
@@ -80,14 +101,14 @@ __device__ __forceinline__ int lane_groups(const QAttnParams& p, int s) {
     return groups_of(start, seq_end(p, start, s));
 }
 __device__ __forceinline__ int wave_scan(int v) {   // inclusive
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int up = __shfl_up(v, o);
-        if (lane >= o) v += up;
-    }
-    return v;
+    v += dpp<0x111>(0, v);             // from 1, 2, 4, 8 lanes in front, within 16
+    v += dpp<0x112>(0, v);
+    v += dpp<0x114>(0, v);
+    v += dpp<0x118>(0, v);
+    v += dpp<0x142, 0xa>(0, v);        // the last of 16 into the next 16, of 32 into the next 32
+    return v + dpp<0x143, 0xc>(0, v);
 }
+__device__ __forceinline__ int last_lane(int v) { return __builtin_amdgcn_readlane(v, 63); }
 
 // Several sequences: a workgroup's piece of the line of groups, and the sequence that it begins in.
 struct Piece {
@@ -102,7 +123,7 @@ __device__ __forceinline__ Piece piece_of(const QAttnParams& p, int j) {
     for (int s0 = 0; s0 < p.n_seq; s0 += 64) {
         mine = lane_groups(p, s0 + lane);
         incl = wave_scan(mine);
-        total += uniform(__shfl(incl, 63));
+        total += last_lane(incl);
     }
     // few groups: one each
     w.begin = total < p.n_wg ? j : (j * total) >> p.log2_wg;
@@ -120,7 +141,7 @@ __device__ __forceinline__ Piece piece_of(const QAttnParams& p, int j) {
             w.before += uniform(__shfl(incl - mine, at));
             return w;
         }
-        w.before += uniform(__shfl(incl, 63));
+        w.before += last_lane(incl);
     }
     w.end = w.begin;   // not reached: the group is on the line
     return w;
@@ -147,14 +168,13 @@ __device__ __forceinline__ void split(float x, bf16_t* part) {
     }
 }
 
-// What a lane holds of 32 keys.  WIDE: head_dim is NB * 128, and a lane's piece of a key is contiguous;
-// otherwise step f takes elements 32 f + 8 g4 .. of a key, nothing beyond head_dim.
-template <int NB>
+// What a lane holds of 32 keys: KE = DP / 4 elements of each of two, VE = DP / 16 of each of eight.
+template <int DP>
 struct Tile {
-    uint32_t kc[2][NB * 4];   // codes of a key's steps
-    uint32_t ks[2][NB * 2];   // their scale bytes: of steps 2 i and 2 i + 1
-    uint32_t vc[NB][8];       // codes of 8 elements of 8 keys
-    u32x2 vs[NB];             // the 8 keys' scale bytes
+    uint32_t kc[2][DP / 32];                 // codes of a key's contraction steps
+    uint32_t ks[2][DP < 256 ? 1 : 2];        // their scale bytes
+    uint32_t vc[8][DP < 256 ? 1 : 2];        // codes of a value's elements
+    u32x2 vs;                                // the 8 values' scale bytes
 };
 
 // Byte `at` of w as a scale: the conversions look at the exponent bits alone, and 255 there is NaN.
@@ -165,151 +185,173 @@ __device__ __forceinline__ uint32_t byte_at(u32x2 w, int at) {
     return (w[at >> 2] >> (at & 3) * 8) & 255u;
 }
 
-template <typename T, int NB, int NC, bool WIDE>
+// A tensor from a uniform address on, for loads with a lane's offset in one register
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t from(const unsigned char* ptr) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(ptr), 0, 0x7fffffff,
+                                             0x00027000);
+}
+
+// DP: 64, 128 or 256, at least head_dim.  EXACT: head_dim is DP, and a lane's piece of a key is contiguous;
+// otherwise step f takes elements 32 f + 8 g4 .. of a key.  Pieces beyond head_dim are read from its
+// beginning: the queries are 0 there, and nobody asks for those outputs.
+template <typename T, int DP, bool EXACT, int NC, bool MULTI>
 __global__ __launch_bounds__(kWaves * 64) void qcache_attn_kernel(QAttnParams p) {
     constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
-    constexpr int F = NB * 4;                      // contraction steps of a score
-    __shared__ f32x4 s_o[kWaves / 2][NC * NB * 8][64];
-    __shared__ float s_m[kWaves][NC * 16], s_l[kWaves][NC * 16];
+    constexpr int F = DP / 32;                     // contraction steps of a score
+    constexpr int VB = DP / 16;                    // output blocks: row i of block f is element VB i + f
+    constexpr bool TWO_AHEAD = DP * NC <= 128;     // where the registers hold three tiles
+    constexpr int kORow = DP + 4;                  // floats of a column's output in LDS
+    extern __shared__ __align__(16) float s_o[];   // [kWaves][16][kORow]
+    __shared__ float2 s_ml[kWaves][16];
 
     const int lane = threadIdx.x & 63;
     const int wave = uniform(threadIdx.x >> 6);
     const int g4 = lane >> 4, l16 = lane & 15;
     const int h = blockIdx.y, tile0 = blockIdx.z * (NC * 16);
-    const int D = WIDE ? NB * 128 : p.D;
+    const int D = EXACT ? DP : p.D;
     const int code_row = D / 2, scale_row = D / kQBlock;
 
     // ---- where a lane's pieces of 32 keys lie ------------------------------------------------
     const int krow = 8 * (l16 >> 2) + (l16 & 3);
-    const uint32_t k_off = (uint32_t)(krow * code_row + g4 * (WIDE ? 16 : 4));
-    const uint32_t ks_off = (uint32_t)(krow * scale_row + (WIDE ? 2 * g4 : g4 >> 1));
-    const uint32_t v_off = (uint32_t)(8 * g4 * code_row + 4 * l16);
-    const uint32_t vs_off = (uint32_t)((g4 * scale_row + (l16 >> 1)) * 8);
-    auto load = [&](int r0, Tile<NB>& t) {          // r0: a multiple of 32 below rows
-        const int64_t row = (int64_t)h * p.rows + r0;
-        const unsigned char* const kc = p.k_codes + row * code_row;
-        const unsigned char* const ks = p.k_scales + row * scale_row;
-        const unsigned char* const vc = p.v_codes + row * code_row;
-        const unsigned char* const vs = p.v_scales + row * scale_row;
+    int k_off[EXACT ? 1 : F], ks_off[EXACT ? 1 : F];
+#pragma unroll
+    for (int f = 0; f < (EXACT ? 1 : F); ++f) {
+        const int d = EXACT ? g4 * (DP / 4) : 32 * f + 8 * g4 < D ? 32 * f + 8 * g4 : 0;
+        k_off[f] = krow * code_row + d / 2;
+        ks_off[f] = krow * scale_row + d / kQBlock;
+    }
+    const int vd = EXACT || l16 * VB < D ? l16 * VB : 0;
+    const int v_off = 8 * g4 * code_row + vd / 2;
+    const int vs_off = (g4 * scale_row + vd / kQBlock) * 8;
+    auto load = [&](int r0, Tile<DP>& t) __attribute__((always_inline)) {
+        const int64_t row = (int64_t)h * p.rows + r0;   // r0: a multiple of 32 below rows
+        const auto kc = from(p.k_codes + row * code_row), ks = from(p.k_scales + row * scale_row);
+        const auto vc = from(p.v_codes + row * code_row), vs = from(p.v_scales + row * scale_row);
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt) {
-            if (WIDE) {
-#pragma unroll
-                for (int nb = 0; nb < NB; ++nb) {
-                    const u32x4 c = *reinterpret_cast<const u32x4*>(kc + kt * 4 * code_row + nb * 64 + k_off);
-#pragma unroll
-                    for (int f = 0; f < 4; ++f) t.kc[kt][nb * 4 + f] = c[f];
-                    t.ks[kt][nb * 2] =
-                        *reinterpret_cast<const uint16_t*>(ks + kt * 4 * scale_row + nb * 8 + ks_off);
-                }
-            } else {
+            const int c0 = kt * 4 * code_row, s0 = kt * 4 * scale_row;
+            if constexpr (!EXACT) {
 #pragma unroll
                 for (int f = 0; f < F; ++f) {
-                    const bool in = 32 * f + 8 * g4 < D;
-                    t.kc[kt][f] = in ? *reinterpret_cast<const uint32_t*>(kc + kt * 4 * code_row + 16 * f + k_off) : 0u;
-                    const uint32_t b = in ? ks[kt * 4 * scale_row + 2 * f + ks_off] : 127u;
-                    if (f & 1) t.ks[kt][f >> 1] |= b << 8;
-                    else t.ks[kt][f >> 1] = b;
+                    t.kc[kt][f] = __builtin_amdgcn_raw_buffer_load_b32(kc, k_off[f], c0, 0);
+                    const uint32_t b = __builtin_amdgcn_raw_buffer_load_b8(ks, ks_off[f], s0, 0);
+                    t.ks[kt][f >> 2] = f & 3 ? t.ks[kt][f >> 2] | b << 8 * (f & 3) : b;
                 }
+            } else if constexpr (DP == 64) {
+                const auto c = __builtin_amdgcn_raw_buffer_load_b64(kc, k_off[0], c0, 0);
+                t.kc[kt][0] = c[0];
+                t.kc[kt][1] = c[1];
+                t.ks[kt][0] = __builtin_amdgcn_raw_buffer_load_b8(ks, ks_off[0], s0, 0);
+            } else {
+#pragma unroll
+                for (int x = 0; x < F; x += 4) {
+                    const auto c = __builtin_amdgcn_raw_buffer_load_b128(kc, k_off[0], c0 + 4 * x, 0);
+#pragma unroll
+                    for (int f = 0; f < 4; ++f) t.kc[kt][x + f] = c[f];
+                }
+                if constexpr (DP == 128)
+                    t.ks[kt][0] = __builtin_amdgcn_raw_buffer_load_b16(ks, ks_off[0], s0, 0);
+                else
+                    t.ks[kt][0] = __builtin_amdgcn_raw_buffer_load_b32(ks, ks_off[0], s0, 0);
             }
         }
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-            const bool in = WIDE || 128 * nb + 8 * l16 < D;
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                t.vc[nb][j] = in ? *reinterpret_cast<const uint32_t*>(vc + j * code_row + nb * 64 + v_off) : 0u;
-            t.vs[nb] = in ? *reinterpret_cast<const u32x2*>(vs + nb * 64 + vs_off)
-                          : u32x2{0x7f7f7f7fu, 0x7f7f7f7fu};
+        for (int j = 0; j < 8; ++j) {
+            if constexpr (DP == 64) {
+                t.vc[j][0] = __builtin_amdgcn_raw_buffer_load_b16(vc, v_off, j * code_row, 0);
+            } else if constexpr (DP == 128) {
+                t.vc[j][0] = __builtin_amdgcn_raw_buffer_load_b32(vc, v_off, j * code_row, 0);
+            } else {
+                const auto c = __builtin_amdgcn_raw_buffer_load_b64(vc, v_off, j * code_row, 0);
+                t.vc[j][0] = c[0];
+                t.vc[j][1] = c[1];
+            }
         }
+        const auto c = __builtin_amdgcn_raw_buffer_load_b64(vs, vs_off, 0, 0);
+        t.vs = u32x2{c[0], c[1]};
     };
 
     // ---- the workgroup's groups ----------------------------------------------------------------
-    const bool single = p.n_seq == 1;
     Piece piece = {0, 0, 0, 0};
-    if (!single) {
+    if constexpr (MULTI) {
         piece = piece_of(p, blockIdx.x);
         if (piece.begin >= piece.end) return;
     }
     for (;;) {
-        const int s = piece.s, start = uniform(seq_start(p, s)), base = (start & ~31) + wave * 32;
-        int g = single ? (int)blockIdx.x : (int)(piece.begin - piece.before);
-        const int g_step = single ? p.n_wg : 1;
-        Tile<NB> cur, next;
-        const int r_first = base + g * kGroup;
-        if (r_first < p.rows) load(r_first, cur);   // whether a row sees it turns out behind the loads
+        const int s = piece.s;
+        const int start = uniform(seq_start(p, s)), base = start & ~31;
+        const int g = MULTI ? (int)(piece.begin - piece.before) : (int)blockIdx.x;
+        const int step = (MULTI ? 1 : p.n_wg) * kGroup;
+        int r0 = base + wave * 32 + g * kGroup;
+        Tile<DP> t0, t1, t2;      // whether a row sees them turns out behind the requests
+        load(min(r0, p.rows - 32), t0);
+        load(min(r0 + step, p.rows - 32), t1);
 
-        // ---- this lane's columns ---------------------------------------------------------------
-        int end[NC], end_min = 0x7fffffff, end_max = start;
+        // ---- this lane's columns (the last one again behind it): queries and what they see ------
+        int end[NC], end_min, end_max, q_at[NC];
+        // the tile's first row, and a lane's row and head as seen from there
+        const int row0 = p.each == 1 ? s : s * p.each + tile0 / p.group;
+        if (p.each == 1) {
+            end_min = end_max = uniform(row_end(p, start, s));
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                end[c] = end_max;
+                q_at[c] = min(tile0 + c * 16 + l16, p.cols - 1);
+            }
+        } else {
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                const int col = min(tile0 + c * 16 + l16, p.cols - 1), in_seq = col / p.group;
+                const int down = s * p.each + in_seq - row0;
+                end[c] = row_end(p, start, row0 + down);
+                q_at[c] = down * p.hq + col - in_seq * p.group;
+                end_min = c ? min(end_min, end[c]) : end[c];
+                end_max = c ? max(end_max, end[c]) : end[c];
+            }
+            end_min = uniform(min16(end_min));
+            end_max = uniform(max16(end_max));
+        }
         bf16x8 qf[NC][PARTS][F];
+        {
+            const T* const q0 = static_cast<const T*>(p.q) + ((int64_t)row0 * p.hq + h * p.group) * D;
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            const int col = tile0 + c * 16 + l16;
-            const bool valid = col < p.cols;
-            const int in_seq = valid ? col / p.group : 0;
-            const int row = s * p.each + in_seq;
-            const int head = h * p.group + (valid ? col - in_seq * p.group : 0);
-            const T* q = static_cast<const T*>(p.q) + ((int64_t)row * p.hq + head) * D;
-            end[c] = valid ? row_end(p, start, row) : start;
-            end_max = max(end_max, end[c]);
-            if (valid) end_min = min(end_min, end[c]);
+            for (int c = 0; c < NC; ++c)
 #pragma unroll
-            for (int f = 0; f < F; ++f) {
-                const int d = WIDE ? (f >> 2) * 128 + 32 * g4 + 8 * (f & 3) : 32 * f + 8 * g4;
-                typedef typename Vec16<T>::type vec_t;
-                vec_t v[8 / Vec16<T>::N] = {};
-                if (valid && (WIDE || d < D))
+                for (int f = 0; f < F; ++f) {
+                    typedef typename Vec16<T>::type vec_t;
+                    const int d = EXACT ? g4 * (DP / 4) + 8 * f : 32 * f + 8 * g4;
+                    const vec_t* q = reinterpret_cast<const vec_t*>(q0 + (uint32_t)(q_at[c] * D + d));
+                    vec_t x[8 / Vec16<T>::N];
 #pragma unroll
-                    for (int i = 0; i < 8 / Vec16<T>::N; ++i)
-                        v[i] = reinterpret_cast<const vec_t*>(q + d)[i];
+                    for (int i = 0; i < 8 / Vec16<T>::N; ++i) x[i] = EXACT || d < D ? q[i] : vec_t{};
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const T x = v[e / Vec16<T>::N][e % Vec16<T>::N];
-                    if constexpr (PARTS == 1) {
-                        qf[c][0][f][e] = x;
-                    } else {
+                    for (int e = 0; e < 8; ++e) {
                         bf16_t part[PARTS];
-                        split<PARTS>(x, part);
+                        if constexpr (PARTS == 1) part[0] = x[0][e];
+                        else split<PARTS>(x[e / 4][e % 4], part);
 #pragma unroll
                         for (int i = 0; i < PARTS; ++i) qf[c][i][f][e] = part[i];
                     }
                 }
-            }
         }
-#pragma unroll
-        for (int o = 8; o > 0; o >>= 1) {
-            end_min = min(end_min, __shfl_xor(end_min, o));
-            end_max = max(end_max, __shfl_xor(end_max, o));
-        }
-        end_min = uniform(end_min);
-        end_max = uniform(end_max);
         // all rows of the sequence have a say in the line's groups, this tile's in the single one's
-        const int groups = single ? groups_of(start, end_max)
-                                  : groups_of(start, uniform(seq_end(p, start, s)));
-        const int g_end = single ? groups : (int)min((int64_t)groups, piece.end - piece.before);
-        if (single && g > 0 && g >= groups) return;
-        const bool whole = !single && g == 0 && g_end == groups;
-        if (!single && blockIdx.y == 0 && blockIdx.z == 0 && threadIdx.x == 0) {
-            if (g == 0) p.held_by[s].x = blockIdx.x;
-            if (g_end == groups) p.held_by[s].y = blockIdx.x;
-        }
+        const int groups = groups_of(start, !MULTI || p.each == 1 ? end_max : uniform(seq_end(p, start, s)));
+        const int g_end = MULTI ? (int)min((int64_t)groups, piece.end - piece.before) : groups;
+        if (!MULTI && g > 0 && g >= groups) return;
+        const bool whole = MULTI ? g == 0 && g_end == groups : p.n_wg == 1;
+        const int r_end = min(end_max, base + g_end * kGroup);
 
         float m2[NC], l[NC];
-        f32x4 o[NC][NB][8];
+        f32x4 o[NC][VB];
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
             m2[c] = -INFINITY;
             l[c] = 0.f;
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-                for (int f = 0; f < 8; ++f) o[c][nb][f] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int f = 0; f < VB; ++f) o[c][f] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
 
-        // ---- the wave's steps, the next one's bytes on their way -----------------------------
-        for (; g < g_end && base + g * kGroup < end_max; g += g_step) {
-            const int r0 = base + g * kGroup, r1 = r0 + g_step * kGroup;
-            if (g + g_step < g_end && r1 < end_max) load(r1, next);
+        auto use = [&](int r0, Tile<DP>& cur) __attribute__((always_inline)) {
             // keys in front of the sequence or behind what some column sees
             const bool edge = r0 < start || r0 + 32 > end_min;
             const int key0 = r0 + 8 * g4;      // of this lane's 8 scores and values
@@ -320,8 +362,8 @@ __global__ __launch_bounds__(kWaves * 64) void qcache_attn_kernel(QAttnParams p)
             for (int f = 0; f < F; ++f)
 #pragma unroll
                 for (int kt = 0; kt < 2; ++kt) {
-                    const float scale = WIDE ? scale_at(cur.ks[kt][(f >> 2) * 2], (f & 3) >> 1)
-                                             : scale_at(cur.ks[kt][f >> 1], f & 1);
+                    const float scale = EXACT ? scale_at(cur.ks[kt][0], f >> 1)
+                                              : scale_at(cur.ks[kt][f >> 2], f & 3);
                     u32x4 w;
 #pragma unroll
                     for (int b = 0; b < 4; ++b) w[b] = cvt2(cur.kc[kt][f], scale, b);
@@ -331,7 +373,7 @@ __global__ __launch_bounds__(kWaves * 64) void qcache_attn_kernel(QAttnParams p)
 #pragma unroll
                         for (int i = PARTS - 1; i >= 0; --i) sc[c][kt] = mfma16(a, qf[c][i][f], sc[c][kt]);
                 }
-            if (edge) {
+            if (__builtin_expect(edge, 0)) {
 #pragma unroll
                 for (int c = 0; c < NC; ++c)
 #pragma unroll
@@ -339,12 +381,9 @@ __global__ __launch_bounds__(kWaves * 64) void qcache_attn_kernel(QAttnParams p)
                         if (key0 + j < start || key0 + j >= end[c]) sc[c][j >> 2][j & 3] = -INFINITY;
                 // what no column sees may be any bytes; its weight is 0, and its scales become 1
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (key0 + j < start || key0 + j >= end_max)
-                            cur.vs[nb][j >> 2] = (cur.vs[nb][j >> 2] & ~(255u << (j & 3) * 8)) |
-                                                 127u << (j & 3) * 8;
+                for (int j = 0; j < 8; ++j)
+                    if (key0 + j < start || key0 + j >= end_max)
+                        cur.vs[j >> 2] = (cur.vs[j >> 2] & ~(255u << (j & 3) * 8)) | 127u << (j & 3) * 8;
             }
             bf16x8 pb[NC][PARTS];
 #pragma unroll
@@ -353,7 +392,7 @@ __global__ __launch_bounds__(kWaves * 64) void qcache_attn_kernel(QAttnParams p)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) top = fmaxf(top, sc[c][j >> 2][j & 3]);
                 top *= p.c2;
-                if (__any(top > m2[c] + 8.f)) {
+                if (__builtin_expect(__any(top > m2[c] + 8.f), 0)) {
                     float m = fmaxf(top, m2[c]);
                     m = fmaxf(m, __shfl_xor(m, 16));
                     m = fmaxf(m, __shfl_xor(m, 32));
@@ -361,9 +400,7 @@ __global__ __launch_bounds__(kWaves * 64) void qcache_attn_kernel(QAttnParams p)
                     m2[c] = m;
                     l[c] *= corr;
 #pragma unroll
-                    for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-                        for (int f = 0; f < 8; ++f) o[c][nb][f] *= corr;
+                    for (int f = 0; f < VB; ++f) o[c][f] *= corr;
                 }
                 const float ref = m2[c] == -INFINITY ? 0.f : m2[c];
 #pragma unroll
@@ -376,159 +413,155 @@ __global__ __launch_bounds__(kWaves * 64) void qcache_attn_kernel(QAttnParams p)
                     for (int i = 0; i < PARTS; ++i) pb[c][i][j] = part[i];
                 }
             }
+            // Scale bytes that stand for NaN: their keys count with another scale, and NaN goes into the
+            // columns that see them by a product of its own (0 times NaN would reach the others).
+            u32x2 vs = cur.vs;
+            const u32x2 nan = ((vs & 0x7f7f7f7fu) + 0x01010101u) & vs & 0x80808080u;
+            if (__builtin_expect(__any((nan[0] | nan[1]) != 0), 0)) {
+                bf16x8 is_nan;
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) {
-                u32x2 vs = cur.vs[nb];
-                // scale bytes that stand for NaN: their keys count with another scale, and NaN goes into the
-                // columns that see them by a product of its own (0 times NaN would reach the others)
-                const u32x2 nan = ((vs & 0x7f7f7f7fu) + 0x01010101u) & vs & 0x80808080u;
-                if (__any((nan[0] | nan[1]) != 0)) {
-                    bf16x8 is_nan;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const bool n = byte_at(vs, j) == kQScaleNan;
-                        is_nan[j] = (bf16_t)(n ? 1.f : 0.f);
-                        if (n) vs[j >> 2] ^= 128u << (j & 3) * 8;
-                    }
-#pragma unroll
-                    for (int c = 0; c < NC; ++c) {
-                        bf16x8 seen;
-#pragma unroll
-                        for (int j = 0; j < 8; ++j)
-                            seen[j] = (bf16_t)(key0 + j >= start && key0 + j < end[c] ? 1.f : 0.f);
-                        const f32x4 n = mfma16(is_nan, seen, f32x4{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if (n[r] > 0.f)
-#pragma unroll
-                                for (int f = 0; f < 8; ++f) o[c][nb][f][r] = __builtin_nanf("");
-                    }
+                for (int j = 0; j < 8; ++j) {
+                    const bool n = byte_at(vs, j) == kQScaleNan;
+                    is_nan[j] = (bf16_t)(n ? 1.f : 0.f);
+                    if (n) vs[j >> 2] ^= 128u << (j & 3) * 8;
                 }
 #pragma unroll
-                for (int b = 0; b < 4; ++b) {
-                    u32x4 lo, hi;
+                for (int c = 0; c < NC; ++c) {
+                    bf16x8 seen;
 #pragma unroll
-                    for (int j = 0; j < 8; j += 2) {
-                        const uint32_t x0 = cvt2(cur.vc[nb][j], scale_at(vs[j >> 2], j & 3), b);
-                        const uint32_t x1 = cvt2(cur.vc[nb][j + 1], scale_at(vs[j >> 2], (j & 3) + 1), b);
-                        lo[j / 2] = __builtin_amdgcn_perm(x1, x0, 0x05040100u);
-                        hi[j / 2] = __builtin_amdgcn_perm(x1, x0, 0x07060302u);
-                    }
-                    const bf16x8 a0 = __builtin_bit_cast(bf16x8, lo), a1 = __builtin_bit_cast(bf16x8, hi);
+                    for (int j = 0; j < 8; ++j)
+                        seen[j] = (bf16_t)(key0 + j >= start && key0 + j < end[c] ? 1.f : 0.f);
+                    const f32x4 n = mfma16(is_nan, seen, f32x4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
-                    for (int c = 0; c < NC; ++c)
+                    for (int r = 0; r < 4; ++r)
+                        if (n[r] > 0.f)
 #pragma unroll
-                        for (int i = PARTS - 1; i >= 0; --i) {
-                            o[c][nb][2 * b] = mfma16(a0, pb[c][i], o[c][nb][2 * b]);
-                            o[c][nb][2 * b + 1] = mfma16(a1, pb[c][i], o[c][nb][2 * b + 1]);
-                        }
+                            for (int f = 0; f < VB; ++f) o[c][f][r] = __builtin_nanf("");
                 }
             }
-            cur = next;
+#pragma unroll
+            for (int f = 0; f < VB; f += 2) {       // a conversion gives elements f and f + 1
+                u32x4 lo, hi;
+#pragma unroll
+                for (int j = 0; j < 8; j += 2) {
+                    const uint32_t x0 = cvt2(cur.vc[j][f >> 3], scale_at(vs[j >> 2], j & 3), (f & 7) / 2);
+                    const uint32_t x1 =
+                        cvt2(cur.vc[j + 1][f >> 3], scale_at(vs[j >> 2], (j & 3) + 1), (f & 7) / 2);
+                    lo[j / 2] = __builtin_amdgcn_perm(x1, x0, 0x05040100u);
+                    hi[j / 2] = __builtin_amdgcn_perm(x1, x0, 0x07060302u);
+                }
+                const bf16x8 a0 = __builtin_bit_cast(bf16x8, lo), a1 = __builtin_bit_cast(bf16x8, hi);
+#pragma unroll
+                for (int c = 0; c < NC; ++c)
+#pragma unroll
+                    for (int i = PARTS - 1; i >= 0; --i) {
+                        o[c][f] = mfma16(a0, pb[c][i], o[c][f]);
+                        o[c][f + 1] = mfma16(a1, pb[c][i], o[c][f + 1]);
+                    }
+            }
+        };
+
+        // ---- the wave's steps, one or two more on their way -----------------------------------------
+        // Behind the last one the loads go on, to rows that are there already: a load that may or may not
+        // have been made would have to be waited for as if it were the one in question.
+        auto load_ahead = [&](Tile<DP>& t) __attribute__((always_inline)) {
+            const int ahead = r0 + 2 * step;
+            load(ahead < r_end ? ahead : r0, t);
+        };
+        for (;;) {
+            if (r0 >= r_end) break;
+            if (TWO_AHEAD) load_ahead(t2);
+            use(r0, t0);
+            if (!TWO_AHEAD) load_ahead(t0);
+            r0 += step;
+            if (r0 >= r_end) break;
+            if (TWO_AHEAD) load_ahead(t0);
+            use(r0, t1);
+            if (!TWO_AHEAD) load_ahead(t1);
+            r0 += step;
+            if (!TWO_AHEAD) continue;
+            if (r0 >= r_end) break;
+            load_ahead(t1);
+            use(r0, t2);
+            r0 += step;
         }
 
-        // ---- the waves meet, always in the same order -----------------------------------------
+        // ---- the waves meet: 16 columns at a time through LDS, a wave per column, always in the same order
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
+            const int left = p.cols - tile0 - c * 16;
+            if (left <= 0) break;
             l[c] += __shfl_xor(l[c], 16);
             l[c] += __shfl_xor(l[c], 32);
-        }
-        __syncthreads();     // the previous sequence's exchange has been read
-        if (g4 == 0)
+            if (MULTI || c) __syncthreads();     // the previous exchange has been read
+            if (l16 < left) {
+                // element VB (4 g4 + r) + f of the column
+                float* const so = s_o + (wave * 16 + l16) * kORow + 4 * VB * g4;
 #pragma unroll
-            for (int c = 0; c < NC; ++c) {
-                s_m[wave][c * 16 + l16] = m2[c];
-                s_l[wave][c * 16 + l16] = l[c];
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int f = 0; f < VB; f += 4)
+                        *reinterpret_cast<f32x4*>(so + VB * r + f) =
+                            f32x4{o[c][f][r], o[c][f + 1][r], o[c][f + 2][r], o[c][f + 3][r]};
+                if (g4 == 0) s_ml[wave][l16] = make_float2(m2[c], l[c]);
             }
-        __syncthreads();
-        float m_all[NC], l_all[NC];
-#pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            float m = -INFINITY;
-#pragma unroll
-            for (int w = 0; w < kWaves; ++w) m = fmaxf(m, s_m[w][c * 16 + l16]);
-            m_all[c] = m;
-            l_all[c] = 0.f;
-            const float ref = m == -INFINITY ? 0.f : m;
-#pragma unroll
-            for (int w = 0; w < kWaves; ++w)
-                l_all[c] += s_l[w][c * 16 + l16] * __builtin_amdgcn_exp2f(s_m[w][c * 16 + l16] - ref);
-            const float mine = __builtin_amdgcn_exp2f(m2[c] - ref);
-#pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-                for (int f = 0; f < 8; ++f) o[c][nb][f] *= mine;
-        }
-#pragma unroll
-        for (int half = kWaves / 2; half > 0; half >>= 1) {
-            if (wave >= half && wave < 2 * half)
-#pragma unroll
-                for (int c = 0; c < NC; ++c)
-#pragma unroll
-                    for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-                        for (int f = 0; f < 8; ++f)
-                            s_o[wave - half][(c * NB + nb) * 8 + f][lane] = o[c][nb][f];
             __syncthreads();
-            if (wave < half)
+            for (int x = wave; x < min(left, 16); x += kWaves) {
+                float m = -INFINITY, sum = 0.f, factor[kWaves];
 #pragma unroll
-                for (int c = 0; c < NC; ++c)
+                for (int w = 0; w < kWaves; ++w) m = fmaxf(m, s_ml[w][x].x);
+                const float ref = m == -INFINITY ? 0.f : m;
 #pragma unroll
-                    for (int nb = 0; nb < NB; ++nb)
+                for (int w = 0; w < kWaves; ++w) {
+                    factor[w] = __builtin_amdgcn_exp2f(s_ml[w][x].x - ref);
+                    sum += s_ml[w][x].y * factor[w];
+                }
+                const int col = tile0 + c * 16 + x;
+                f32x2 a[DP > 128 ? 2 : 1];
 #pragma unroll
-                        for (int f = 0; f < 8; ++f)
-                            o[c][nb][f] += s_o[wave][(c * NB + nb) * 8 + f][lane];
-            if (half > 1) __syncthreads();
-        }
-        if (wave == 0) {
+                for (int i = 0; i < (DP > 128 ? 2 : 1); ++i) {
+                    a[i] = f32x2{0.f, 0.f};
+                    const int d = DP < 128 ? 2 * (lane & 31) : 2 * lane + 128 * i;
 #pragma unroll
-            for (int c = 0; c < NC; ++c) {
-                const int col = tile0 + c * 16 + l16;
-                if (col >= p.cols) continue;
-                const int in_seq = col / p.group;
-                const int64_t oc = (int64_t)(s * p.each + in_seq) * p.hq + h * p.group +
-                                   (col - in_seq * p.group);
-                // all of the row's keys are here
-                const bool direct = single ? p.n_wg == 1 || groups_of(start, end[c]) <= 1 : whole;
-                if (direct && single && blockIdx.x) continue;
-                const int64_t part =
-                    ((int64_t)(single ? blockIdx.x : blockIdx.x + s) * p.hkv + h) * p.cols + col;
-                const float inv = l_all[c] == 0.f ? 0.f : 1.f / l_all[c];
-#pragma unroll
-                for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int d = nb * 128 + 8 * (4 * g4 + r);
-                        if (!WIDE && d >= D) continue;
-                        if (direct) {
-                            T* op = static_cast<T*>(p.out) + oc * D + d;
-#pragma unroll
-                            for (int e = 0; e < 8; e += Vec16<T>::N) {
-                                typename Vec16<T>::type v;
-#pragma unroll
-                                for (int i = 0; i < Vec16<T>::N; ++i)
-                                    v[i] = Elem<T>::from_f32(o[c][nb][e + i][r] * inv);
-                                *reinterpret_cast<typename Vec16<T>::type*>(op + e) = v;
-                            }
-                        } else {
-                            float* op = p.part_o + part * D + d;
-#pragma unroll
-                            for (int e = 0; e < 8; e += 4)
-                                *reinterpret_cast<f32x4*>(op + e) =
-                                    f32x4{o[c][nb][e][r], o[c][nb][e + 1][r], o[c][nb][e + 2][r],
-                                          o[c][nb][e + 3][r]};
-                        }
+                    for (int w = 0; w < kWaves; ++w) {
+                        const f32x2 v = *reinterpret_cast<const f32x2*>(s_o + (w * 16 + x) * kORow + d);
+                        a[i][0] += v[0] * factor[w];
+                        a[i][1] += v[1] * factor[w];
                     }
-                if (g4 == 0) {
-                    if (!direct) p.part_ml[part] = make_float2(m_all[c], l_all[c]);
-                    else if (p.lse)
-                        p.lse[oc] = l_all[c] == 0.f ? -INFINITY
-                                                    : (m_all[c] + __builtin_amdgcn_logf(l_all[c])) *
-                                                          0.69314718055994531f;
+                }
+                if (whole) {
+                    const int in_seq = p.each == 1 ? 0 : col / p.group;
+                    const int64_t oc = (int64_t)(s * p.each + in_seq) * p.hq + h * p.group +
+                                       (col - in_seq * p.group);
+                    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+                    for (int i = 0; i < (DP > 128 ? 2 : 1); ++i) {
+                        const int d = 2 * lane + 128 * i;
+                        if (d >= D) break;
+                        typedef T pair_t __attribute__((ext_vector_type(2)));
+                        *reinterpret_cast<pair_t*>(static_cast<T*>(p.out) + oc * D + d) =
+                            pair_t{Elem<T>::from_f32(a[i][0] * inv), Elem<T>::from_f32(a[i][1] * inv)};
+                    }
+                    if (lane == 0 && p.lse)
+                        p.lse[oc] = sum == 0.f ? -INFINITY
+                                               : (m + __builtin_amdgcn_logf(sum)) * kLn2;
+                } else {
+                    const int64_t part =
+                        ((int64_t)(MULTI ? blockIdx.x + s : blockIdx.x) * p.hkv + h) * p.cols + col;
+#pragma unroll
+                    for (int i = 0; i < (DP > 128 ? 2 : 1); ++i) {
+                        const int d = 2 * lane + 128 * i;
+                        if (d < D) *reinterpret_cast<f32x2*>(p.part_o + part * D + d) = a[i];
+                    }
+                    if (lane == 0) p.part_ml[part] = make_float2(m, sum);
                 }
             }
         }
-        if (single) return;
+        if constexpr (!MULTI) return;
+        if (blockIdx.y == 0 && blockIdx.z == 0 && threadIdx.x == 0) {
+            if (g == 0) p.held_by[s].x = blockIdx.x;
+            if (g_end == groups) p.held_by[s].y = blockIdx.x;
+        }
         piece.begin = piece.before + g_end;
         if (piece.begin >= piece.end) return;
         piece.before += groups;
@@ -551,8 +584,8 @@ __global__ __launch_bounds__(kJoinWaves * 64) void qcache_attn_join_kernel(QAttn
     T* out = static_cast<T*>(p.out) + oc * p.D;
     const int start = uniform(seq_start(p, s));
     int j0 = 0, j1, slot0 = 0;
-    if (p.n_seq == 1) {
-        j1 = min(p.n_wg, groups_of(start, uniform(row_end(p, start, row)))) - 1;
+    if (p.n_seq == 1) {                   // the first workgroup has a part even where there is no key
+        j1 = max(0, min(p.n_wg, groups_of(start, uniform(row_end(p, start, row)))) - 1);
     } else {
         if (seq_end(p, start, s) == start) {
             if ((int)threadIdx.x < p.D) out[threadIdx.x] = Elem<T>::from_f32(0.f);
@@ -563,8 +596,8 @@ __global__ __launch_bounds__(kJoinWaves * 64) void qcache_attn_join_kernel(QAttn
         j0 = uniform(by.x);
         j1 = uniform(by.y);
         slot0 = s;
+        if (j1 <= j0) return;             // written by the workgroup that held it all
     }
-    if (j1 <= j0) return;                 // written by the workgroup that held it all
     const int h = head / p.group, col = (row - s * p.each) * p.group + head % p.group;
     const int64_t slot_rows = (int64_t)p.hkv * p.cols;
     const int64_t first = (int64_t)slot0 * slot_rows + (int64_t)h * p.cols + col;
@@ -617,19 +650,46 @@ __global__ __launch_bounds__(kJoinWaves * 64) void qcache_attn_join_kernel(QAttn
     }
     out[d] = Elem<T>::from_f32(sum == 0.f ? 0.f : a / sum);
     if (d == 0 && p.lse)
-        p.lse[oc] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f;
+        p.lse[oc] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
-template <typename T, int NB, int NC>
-void launch_main(const QAttnParams& p, bool wide, dim3 grid, hipStream_t st) {
-    if (wide)
-        hipLaunchKernelGGL((qcache_attn_kernel<T, NB, NC, true>), grid, dim3(kWaves * 64), 0, st, p);
-    else
-        hipLaunchKernelGGL((qcache_attn_kernel<T, NB, NC, false>), grid, dim3(kWaves * 64), 0, st, p);
+template <typename T, int DP, bool EXACT, int NC, bool MULTI>
+pkv_status launch_kernel(const QAttnParams& p, dim3 grid, hipStream_t st) {
+    constexpr int kBytes = kWaves * 16 * (DP + 4) * sizeof(float);
+    auto* const kernel = &qcache_attn_kernel<T, DP, EXACT, NC, MULTI>;
+    static std::atomic<bool> configured{false};   // set twice at worst: the calls are idempotent
+    if (!configured.load(std::memory_order_acquire)) {
+        if (hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                                hipFuncAttributeMaxDynamicSharedMemorySize, kBytes) != hipSuccess)
+            return PKV_ERR_LAUNCH;
+        configured.store(true, std::memory_order_release);
+    }
+    hipLaunchKernelGGL(kernel, grid, dim3(kWaves * 64), kBytes, st, p);
+    return launch_status();
+}
+template <typename T, int DP, int NC>
+pkv_status launch_main(const QAttnParams& p, dim3 grid, hipStream_t st) {
+    const bool multi = p.n_seq > 1;
+    return p.D == DP ? (multi ? launch_kernel<T, DP, true, NC, true>(p, grid, st)
+                              : launch_kernel<T, DP, true, NC, false>(p, grid, st))
+                     : (multi ? launch_kernel<T, DP, false, NC, true>(p, grid, st)
+                              : launch_kernel<T, DP, false, NC, false>(p, grid, st));
+}
+template <typename T>
+pkv_status launch_main(const QAttnParams& p, int nc, dim3 grid, hipStream_t st) {
+    if (p.D > 128) return launch_main<T, 256, 1>(p, grid, st);
+    if (p.D > 64) {
+        if constexpr (sizeof(T) == 2)
+            if (nc == 2) return launch_main<T, 128, 2>(p, grid, st);
+        return launch_main<T, 128, 1>(p, grid, st);
+    }
+    if constexpr (sizeof(T) == 2)
+        if (nc == 2) return launch_main<T, 64, 2>(p, grid, st);
+    return launch_main<T, 64, 1>(p, grid, st);
 }
 
 struct QPlan {
-    int nb, nc, log2_wg;
+    int nc, log2_wg;
     int64_t tiles;
     size_t parts;
 };
@@ -637,14 +697,14 @@ struct QPlan {
 QPlan plan(const pkv_layer_cfg& cfg, int64_t rows, int64_t m, int64_t n_seq) {
     QPlan pl;
     const int64_t cols = m / n_seq * (cfg.n_q_heads / cfg.n_kv_heads);
-    pl.nb = cfg.head_dim > 128 ? 2 : 1;
     // columns of a workgroup: as many as there are, up to what the registers hold
-    const int most = (cfg.dtype == PKV_F32 ? 2 : 4) / pl.nb;
-    pl.nc = cols <= 16 || most == 1 ? 1 : cols <= 32 || most == 2 ? 2 : 4;
+    pl.nc = cols <= 16 || cfg.dtype == PKV_F32 || cfg.head_dim > 128 ? 1 : 2;
     pl.tiles = ceil_div(cols, 16 * pl.nc);
-    // about two workgroups per CU, and no more than there can be groups
-    const int64_t want = std::min(512 / std::max<int64_t>(1, cfg.n_kv_heads * pl.tiles),
-                                  (ceil_div(rows, kGroup) + 1) * n_seq);
+    // about a workgroup per CU, and no more than there can be groups; one for a short cache, whose
+    // few steps in a row cost less than a second launch
+    int64_t want = std::min(256 / std::max<int64_t>(1, cfg.n_kv_heads * pl.tiles),
+                            (ceil_div(rows, kGroup) + 1) * n_seq);
+    if (n_seq == 1 && rows <= 8 * kGroup) want = 1;
     pl.log2_wg = 0;
     while ((2 << pl.log2_wg) <= want) ++pl.log2_wg;
     pl.parts = (size_t)((1 << pl.log2_wg) + (n_seq > 1 ? n_seq : 0)) * cfg.n_kv_heads * cols;
@@ -689,22 +749,11 @@ pkv_status launch_qcache_attn(const pkv_layer_cfg& cfg, const void* q, const pkv
     p.n_wg = 1 << pl.log2_wg;
     p.log2_wg = pl.log2_wg;
     p.c2 = scale * 1.4426950408889634f;
-    const bool bf16 = cfg.dtype == PKV_BF16, wide = cfg.head_dim == 128 * pl.nb;
+    const bool bf16 = cfg.dtype == PKV_BF16;
     const dim3 grid((unsigned)p.n_wg, (unsigned)cfg.n_kv_heads, (unsigned)pl.tiles);
-    if (bf16 && pl.nb == 1) {
-        if (pl.nc == 1) launch_main<bf16_t, 1, 1>(p, wide, grid, st);
-        else if (pl.nc == 2) launch_main<bf16_t, 1, 2>(p, wide, grid, st);
-        else launch_main<bf16_t, 1, 4>(p, wide, grid, st);
-    } else if (bf16) {
-        if (pl.nc == 1) launch_main<bf16_t, 2, 1>(p, wide, grid, st);
-        else launch_main<bf16_t, 2, 2>(p, wide, grid, st);
-    } else if (pl.nb == 1) {
-        if (pl.nc == 1) launch_main<float, 1, 1>(p, wide, grid, st);
-        else launch_main<float, 1, 2>(p, wide, grid, st);
-    } else {
-        launch_main<float, 2, 1>(p, wide, grid, st);
-    }
-    if (launch_status() != PKV_OK) return PKV_ERR_LAUNCH;
+    const pkv_status status = bf16 ? launch_main<bf16_t>(p, pl.nc, grid, st)
+                                   : launch_main<float>(p, pl.nc, grid, st);
+    if (status != PKV_OK) return status;
     if (n_seq == 1 && p.n_wg == 1) return PKV_OK;
     const dim3 rows_heads((unsigned)(m * cfg.n_q_heads));
     if (bf16)
