@@ -579,11 +579,36 @@ def pkv_query_score_lse(cfg: LayerCfg, q: torch.Tensor, k: torch.Tensor, lse: to
 
 # ---- packed prompts, the cache in 4 bits -------------------------------------------
 
-def _current(*tensors: Optional[torch.Tensor]) -> None:
-    """The calls run on the current device: their tensors have to be its own."""
-    devices = {t.get_device() for t in tensors if t is not None}
-    if devices != {torch.cuda.current_device()}:
-        raise ValueError("all tensors must be on the current device")
+# These calls run on the current device and refuse tensors of another one; one look at a tensor's
+# device serves both checks (the binding's time is of the order of a small launch).
+def _device_of_call(t: torch.Tensor) -> int:
+    return torch.cuda.current_device() if t.is_cuda else -2
+
+
+# the same number without a look at whether CUDA is initialised: t is on the GPU
+if hasattr(torch._C, "_cuda_getDevice"):
+    def _device_of_call(t: torch.Tensor) -> int:   # noqa: F811
+        return torch._C._cuda_getDevice() if t.is_cuda else -2
+
+
+def _own(t: Optional[torch.Tensor], dtype: torch.dtype, name: str, device: int):
+    if t is None:
+        return None
+    if t.get_device() != device:
+        raise ValueError(f"{name} must be a GPU tensor of the current device")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must have dtype {dtype}, got {t.dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _own_ws(ws: Optional[torch.Tensor], device: int):
+    if ws is None:
+        return None, 0
+    if ws.get_device() != device or not ws.is_contiguous():
+        raise ValueError("workspace must be a contiguous GPU tensor of the current device")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
 
 
 def pkv_packed_attn_workspace_bytes(cfg: LayerCfg, m: int) -> int:
@@ -594,20 +619,19 @@ def pkv_packed_attn(cfg: LayerCfg, q: torch.Tensor, k: torch.Tensor, v: torch.Te
                     row_pos: torch.Tensor, out: torch.Tensor,
                     lse_out: Optional[torch.Tensor] = None, softmax_scale: float = 0.0,
                     ws: Optional[torch.Tensor] = None) -> None:
-    m, dt = row_pos.shape[0], cfg.torch_dtype
-    if row_pos.dim() != 1 or q.shape != (m, cfg.n_q_heads, cfg.head_dim) or out.shape != q.shape:
+    m, hq, d, dt = q.shape[0], cfg.n_q_heads, cfg.head_dim, cfg.torch_dtype
+    if row_pos.shape != (m,) or q.shape != (m, hq, d) or out.shape != q.shape:
         raise ValueError("q/out must be [m, Hq, D], row_pos [m]")
-    if k.shape != (m, cfg.n_kv_heads, cfg.head_dim) or v.shape != k.shape:
+    if k.shape != (m, cfg.n_kv_heads, d) or v.shape != k.shape:
         raise ValueError("k/v must be [m, Hkv, D]")
-    if lse_out is not None and lse_out.shape != (m, cfg.n_q_heads):
+    if lse_out is not None and lse_out.shape != (m, hq):
         raise ValueError("lse_out must be [m, Hq]")
-    ptrs = (_ptr(q, dt, "q"), _ptr(k, dt, "k"), _ptr(v, dt, "v"),
-            _ptr(row_pos, torch.int32, "row_pos"), _ptr(out, dt, "out"),
-            _ptr(lse_out, torch.float32, "lse_out"))
-    wp, wb = _ws(ws)
-    _current(q, k, v, row_pos, out, lse_out, ws)
+    dev = _device_of_call(q)
+    wp, wb = _own_ws(ws, dev)
     _check("pkv_packed_attn", load_library().pkv_packed_attn(
-        cfg._ref, *ptrs, m, float(softmax_scale), wp, wb, _stream()))
+        cfg._ref, _own(q, dt, "q", dev), _own(k, dt, "k", dev), _own(v, dt, "v", dev),
+        _own(row_pos, torch.int32, "row_pos", dev), _own(out, dt, "out", dev),
+        _own(lse_out, torch.float32, "lse_out", dev), m, softmax_scale, wp, wb, _stream()))
 
 
 class QCache:
@@ -628,7 +652,8 @@ class QCache:
                 raise ValueError(f"{name} must be {list(shape)}")
         self._c = _CQCache(*(_ptr(t, torch.uint8, name) for name, t in self.tensors.items()),
                            self.rows)
-        if len({t.get_device() for t in self.tensors.values()}) != 1:
+        self.device = k_codes.get_device()
+        if any(t.get_device() != self.device for t in self.tensors.values()):
             raise ValueError("all tensors of a cache must be on one device")
         self._ref = ctypes.byref(self._c)
 
@@ -646,10 +671,12 @@ class QCache:
                           for s in shapes.values()))
 
 
-def _of_cache(cfg: LayerCfg, cache: QCache) -> torch.Tensor:
-    if (cache.heads, cache.head_dim) != (cfg.n_kv_heads, cfg.head_dim):
+def _of_cache(cfg: LayerCfg, cache: QCache, device: int):
+    if cache.heads != cfg.n_kv_heads or cache.head_dim != cfg.head_dim:
         raise ValueError("the cache was made for other heads")
-    return cache.tensors["k_codes"]
+    if cache.device != device:
+        raise ValueError("the cache must be on the GPU that is the current device")
+    return cache._ref
 
 
 def pkv_qcache_store(cfg: LayerCfg, k: torch.Tensor, v: torch.Tensor, cache: QCache,
@@ -659,11 +686,10 @@ def pkv_qcache_store(cfg: LayerCfg, k: torch.Tensor, v: torch.Tensor, cache: QCa
         raise ValueError("k/v must be [m, Hkv, D]")
     if dst_row is not None and dst_row.shape != (m,):
         raise ValueError("dst_row must be [m]")
-    own = _of_cache(cfg, cache)
-    ptrs = (_ptr(k, dt, "k"), _ptr(v, dt, "v"), _ptr(dst_row, torch.int32, "dst_row"))
-    _current(k, v, dst_row, own)
+    dev = _device_of_call(k)
     _check("pkv_qcache_store", load_library().pkv_qcache_store(
-        cfg._ref, *ptrs, cache._ref, m, _stream()))
+        cfg._ref, _own(k, dt, "k", dev), _own(v, dt, "v", dev),
+        _own(dst_row, torch.int32, "dst_row", dev), _of_cache(cfg, cache, dev), m, _stream()))
 
 
 def pkv_qcache_restore(cfg: LayerCfg, cache: QCache, k_out: torch.Tensor, v_out: torch.Tensor,
@@ -673,15 +699,15 @@ def pkv_qcache_restore(cfg: LayerCfg, cache: QCache, k_out: torch.Tensor, v_out:
     m, dt = k_out.shape[0], cfg.torch_dtype
     if k_out.shape != (m, cfg.n_kv_heads, cfg.head_dim) or v_out.shape != k_out.shape:
         raise ValueError("k_out/v_out must be [m, Hkv, D]")
-    for t, name in ((row_idx, "row_idx"), (pos, "pos")):
-        if t is not None and t.shape != (m,):
-            raise ValueError(f"{name} must be [m]")
-    own = _of_cache(cfg, cache)
-    ptrs = (_ptr(row_idx, torch.int32, "row_idx"), _ptr(pos, torch.int32, "pos"))
-    outs = (_ptr(k_out, dt, "k_out"), _ptr(v_out, dt, "v_out"))
-    _current(k_out, v_out, row_idx, pos, own)
+    if row_idx is not None and row_idx.shape != (m,):
+        raise ValueError("row_idx must be [m]")
+    if pos is not None and pos.shape != (m,):
+        raise ValueError("pos must be [m]")
+    dev = _device_of_call(k_out)
     _check("pkv_qcache_restore", load_library().pkv_qcache_restore(
-        cfg._ref, cache._ref, *ptrs, int(pos_base), int(bool(rotate)), *outs, m, _stream()))
+        cfg._ref, _of_cache(cfg, cache, dev), _own(row_idx, torch.int32, "row_idx", dev),
+        _own(pos, torch.int32, "pos", dev), int(pos_base), bool(rotate),
+        _own(k_out, dt, "k_out", dev), _own(v_out, dt, "v_out", dev), m, _stream()))
 
 
 def pkv_qcache_attn_workspace_bytes(cfg: LayerCfg, rows: int, m: int, n_seq: int = 1) -> int:
@@ -693,21 +719,20 @@ def pkv_qcache_attn(cfg: LayerCfg, q: torch.Tensor, cache: QCache, row_pos: torc
                     out: torch.Tensor, seq_start: Optional[torch.Tensor] = None, n_seq: int = 1,
                     lse_out: Optional[torch.Tensor] = None, softmax_scale: float = 0.0,
                     ws: Optional[torch.Tensor] = None) -> None:
-    m, dt = row_pos.shape[0], cfg.torch_dtype
-    if row_pos.dim() != 1 or q.shape != (m, cfg.n_q_heads, cfg.head_dim) or out.shape != q.shape:
+    m, hq, d, dt = q.shape[0], cfg.n_q_heads, cfg.head_dim, cfg.torch_dtype
+    if row_pos.shape != (m,) or q.shape != (m, hq, d) or out.shape != q.shape:
         raise ValueError("q/out must be [m, Hq, D], row_pos [m]")
     if seq_start is not None and seq_start.shape != (n_seq,):
         raise ValueError("seq_start must be [n_seq]")
-    if lse_out is not None and lse_out.shape != (m, cfg.n_q_heads):
+    if lse_out is not None and lse_out.shape != (m, hq):
         raise ValueError("lse_out must be [m, Hq]")
-    own = _of_cache(cfg, cache)
-    qp = _ptr(q, dt, "q")
-    ptrs = (_ptr(row_pos, torch.int32, "row_pos"), _ptr(seq_start, torch.int32, "seq_start"),
-            _ptr(out, dt, "out"), _ptr(lse_out, torch.float32, "lse_out"))
-    wp, wb = _ws(ws)
-    _current(q, row_pos, seq_start, out, lse_out, ws, own)
+    dev = _device_of_call(q)
+    wp, wb = _own_ws(ws, dev)
     _check("pkv_qcache_attn", load_library().pkv_qcache_attn(
-        cfg._ref, qp, cache._ref, *ptrs, m, int(n_seq), float(softmax_scale), wp, wb, _stream()))
+        cfg._ref, _own(q, dt, "q", dev), _of_cache(cfg, cache, dev),
+        _own(row_pos, torch.int32, "row_pos", dev),
+        _own(seq_start, torch.int32, "seq_start", dev), _own(out, dt, "out", dev),
+        _own(lse_out, torch.float32, "lse_out", dev), m, n_seq, softmax_scale, wp, wb, _stream()))
 
 
 # ---- layer glue -------------------------------------------------------------------

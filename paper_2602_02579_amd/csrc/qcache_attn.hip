@@ -86,19 +86,23 @@ __device__ __forceinline__ int end_of(const QAttnParams& p, int start, int pos) 
 __device__ __forceinline__ int row_end(const QAttnParams& p, int start, int row) {
     return end_of(p, start, p.row_pos[row]);
 }
-__device__ __forceinline__ int seq_end(const QAttnParams& p, int start, int s) {
-    int end = start;
-    for (int r = 0; r < p.each; ++r) end = max(end, row_end(p, start, s * p.each + r));
-    return end;
-}
 // groups are counted from the 32 rows that hold the first one
 __device__ __forceinline__ int groups_of(int start, int end) {
     return end > start ? (end - (start & ~31) + kGroup - 1) / kGroup : 0;
 }
-__device__ __forceinline__ int lane_groups(const QAttnParams& p, int s) {
-    if (s >= p.n_seq) return 0;
-    const int start = seq_start(p, s);
-    return groups_of(start, seq_end(p, start, s));
+// A sequence's first row and the groups that its rows see together
+struct Seq {
+    int start, groups;
+};
+__device__ __forceinline__ Seq seq_of(const QAttnParams& p, int s) {
+    const int32_t* const row_pos = p.row_pos + (int64_t)s * p.each;
+    const int given = p.seq_start ? p.seq_start[s] : 0;
+    int pos = row_pos[0];
+    for (int r = 1; r < p.each; r += 4)       // four at once
+#pragma unroll
+        for (int i = 0; i < 4; ++i) pos = max(pos, row_pos[min(r + i, p.each - 1)]);
+    const int start = start_in_cache(p, given);
+    return {start, groups_of(start, end_of(p, start, pos))};
 }
 __device__ __forceinline__ int wave_scan(int v) {   // inclusive
     v += dpp<0x111>(0, v);             // from 1, 2, 4, 8 lanes in front, within 16
@@ -110,19 +114,24 @@ __device__ __forceinline__ int wave_scan(int v) {   // inclusive
 }
 __device__ __forceinline__ int last_lane(int v) { return __builtin_amdgcn_readlane(v, 63); }
 
-// Several sequences: a workgroup's piece of the line of groups, and the sequence that it begins in.
+// Several sequences: a workgroup's piece of the line of groups, and the sequence that it is in.
 struct Piece {
     int64_t begin, end, before;   // before: groups in front of sequence s
     int s;
+    Seq seq;                      // of sequence s
+    Seq of_lane;                  // up to 64 sequences: of the one of the lane's number
 };
+__device__ __forceinline__ Seq lane_seq(const QAttnParams& p, int s) {
+    return s < p.n_seq ? seq_of(p, s) : Seq{0, 0};
+}
 __device__ __forceinline__ Piece piece_of(const QAttnParams& p, int j) {
     const int lane = threadIdx.x & 63;
-    Piece w = {0, 0, 0, 0};
+    Piece w = {};
     int64_t total = 0;
-    int incl = 0, mine = 0;
+    int incl = 0;
     for (int s0 = 0; s0 < p.n_seq; s0 += 64) {
-        mine = lane_groups(p, s0 + lane);
-        incl = wave_scan(mine);
+        w.of_lane = lane_seq(p, s0 + lane);
+        incl = wave_scan(w.of_lane.groups);
         total += last_lane(incl);
     }
     // few groups: one each
@@ -131,20 +140,38 @@ __device__ __forceinline__ Piece piece_of(const QAttnParams& p, int j) {
     if (w.begin >= w.end) return w;
     for (int s0 = 0; s0 < p.n_seq; s0 += 64) {
         if (p.n_seq > 64) {
-            mine = lane_groups(p, s0 + lane);
-            incl = wave_scan(mine);
+            w.of_lane = lane_seq(p, s0 + lane);
+            incl = wave_scan(w.of_lane.groups);
         }
         const uint64_t past = __ballot(w.before + incl > w.begin);
         if (past) {
             const int at = __builtin_ctzll(past);
             w.s = s0 + at;
-            w.before += uniform(__shfl(incl - mine, at));
+            w.seq.start = __builtin_amdgcn_readlane(w.of_lane.start, at);
+            w.seq.groups = __builtin_amdgcn_readlane(w.of_lane.groups, at);
+            w.before += __builtin_amdgcn_readlane(incl, at) - w.seq.groups;
             return w;
         }
         w.before += last_lane(incl);
     }
     w.end = w.begin;   // not reached: the group is on the line
     return w;
+}
+// The next sequence that has groups; false: there is none
+__device__ __forceinline__ bool next_sequence(const QAttnParams& p, Piece& w) {
+    w.before += w.seq.groups;
+    while (++w.s < p.n_seq) {
+        if (p.n_seq <= 64) {
+            w.seq.start = __builtin_amdgcn_readlane(w.of_lane.start, w.s);
+            w.seq.groups = __builtin_amdgcn_readlane(w.of_lane.groups, w.s);
+        } else {
+            const Seq q = seq_of(p, w.s);
+            w.seq.start = uniform(q.start);
+            w.seq.groups = uniform(q.groups);
+        }
+        if (w.seq.groups) return true;
+    }
+    return false;
 }
 
 __device__ __forceinline__ uint32_t cvt2(uint32_t codes, float scale, int byte) {
@@ -272,14 +299,15 @@ __global__ __launch_bounds__(kWaves * 64) void qcache_attn_kernel(QAttnParams p)
     };
 
     // ---- the workgroup's groups ----------------------------------------------------------------
-    Piece piece = {0, 0, 0, 0};
+    Piece piece = {};
     if constexpr (MULTI) {
         piece = piece_of(p, blockIdx.x);
         if (piece.begin >= piece.end) return;
     }
     for (;;) {
         const int s = piece.s;
-        const int start = uniform(seq_start(p, s)), base = start & ~31;
+        const int start = MULTI ? piece.seq.start : uniform(p.seq_start ? start_in_cache(p, *p.seq_start) : 0);
+        const int base = start & ~31;
         const int g = MULTI ? (int)(piece.begin - piece.before) : (int)blockIdx.x;
         const int step = (MULTI ? 1 : p.n_wg) * kGroup;
         int r0 = base + wave * 32 + g * kGroup;
@@ -335,7 +363,7 @@ __global__ __launch_bounds__(kWaves * 64) void qcache_attn_kernel(QAttnParams p)
                 }
         }
         // all rows of the sequence have a say in the line's groups, this tile's in the single one's
-        const int groups = groups_of(start, !MULTI || p.each == 1 ? end_max : uniform(seq_end(p, start, s)));
+        const int groups = MULTI ? piece.seq.groups : groups_of(start, end_max);
         const int g_end = MULTI ? (int)min((int64_t)groups, piece.end - piece.before) : groups;
         if (!MULTI && g > 0 && g >= groups) return;
         const bool whole = MULTI ? g == 0 && g_end == groups : p.n_wg == 1;
@@ -563,11 +591,7 @@ __global__ __launch_bounds__(kWaves * 64) void qcache_attn_kernel(QAttnParams p)
             if (g_end == groups) p.held_by[s].y = blockIdx.x;
         }
         piece.begin = piece.before + g_end;
-        if (piece.begin >= piece.end) return;
-        piece.before += groups;
-        do ++piece.s;                       // a group is left: one of them holds it
-        while (piece.s < p.n_seq && uniform(lane_groups(p, piece.s)) == 0);
-        if (piece.s >= p.n_seq) return;
+        if (piece.begin >= piece.end || !next_sequence(p, piece)) return;
     }
 }
 
@@ -582,52 +606,54 @@ __global__ __launch_bounds__(kJoinWaves * 64) void qcache_attn_join_kernel(QAttn
     const int row = (int)(oc / p.hq), head = (int)(oc % p.hq);
     const int s = row / p.each;
     T* out = static_cast<T*>(p.out) + oc * p.D;
-    const int start = uniform(seq_start(p, s));
-    int j0 = 0, j1, slot0 = 0;
-    if (p.n_seq == 1) {                   // the first workgroup has a part even where there is no key
-        j1 = max(0, min(p.n_wg, groups_of(start, uniform(row_end(p, start, row)))) - 1);
-    } else {
-        if (seq_end(p, start, s) == start) {
+    const bool single = p.n_seq == 1;
+    const int h = head / p.group, col = (row - s * p.each) * p.group + head % p.group;
+    const int64_t slot_rows = (int64_t)p.hkv * p.cols;
+    const int64_t first = (int64_t)(single ? 0 : s) * slot_rows + (int64_t)h * p.cols + col;
+    int2 by = {0, p.n_wg - 1};            // one sequence: the parts are requested before it is known
+    if (!single) {                        // how many there are
+        by = p.held_by[s];
+        if (seq_of(p, s).groups == 0) {
             if ((int)threadIdx.x < p.D) out[threadIdx.x] = Elem<T>::from_f32(0.f);
             if (threadIdx.x == 0 && p.lse) p.lse[oc] = -INFINITY;
             return;
         }
-        const int2 by = p.held_by[s];
-        j0 = uniform(by.x);
-        j1 = uniform(by.y);
-        slot0 = s;
-        if (j1 <= j0) return;             // written by the workgroup that held it all
+        if (by.y <= by.x) return;         // written by the workgroup that held it all
     }
-    const int h = head / p.group, col = (row - s * p.each) * p.group + head % p.group;
-    const int64_t slot_rows = (int64_t)p.hkv * p.cols;
-    const int64_t first = (int64_t)slot0 * slot_rows + (int64_t)h * p.cols + col;
+    const int j0 = uniform(by.x), j_most = uniform(by.y);
     float acc[4] = {0.f, 0.f, 0.f, 0.f}, l = 0.f, m = -INFINITY;
-    for (int j = j0 + wave; j <= j1; j += 8 * kJoinWaves) {
-        float2 ml[8];
-        float x[8][4];
+    int j1 = j_most;
+    for (int j = j0 + wave; j <= j1; j += 4 * kJoinWaves) {
+        float2 ml[4];
+        float x[4][4];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {          // eight parts at once
-            const bool in = j + u * kJoinWaves <= j1;
-            const int64_t at = first + (in ? j + u * kJoinWaves : j) * slot_rows;
+        for (int u = 0; u < 4; ++u) {          // four parts at once
+            const int64_t at = first + min(j + u * kJoinWaves, j_most) * slot_rows;
             ml[u] = p.part_ml[at];
-            if (!in) ml[u] = make_float2(-INFINITY, 0.f);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 x[u][i] = lane + 64 * i < p.D ? p.part_o[at * p.D + lane + 64 * i] : 0.f;
         }
+        if (single) {                          // the first workgroup has a part even where there is no key
+            const int start = p.seq_start ? start_in_cache(p, *p.seq_start) : 0;
+            j1 = min(j_most, max(0, uniform(groups_of(start, row_end(p, start, row))) - 1));
+        }
         float mn = m;
 #pragma unroll
-        for (int u = 0; u < 8; ++u) mn = fmaxf(mn, ml[u].x);
+        for (int u = 0; u < 4; ++u) {
+            if (j + u * kJoinWaves > j1) ml[u] = make_float2(-INFINITY, 0.f);
+            mn = fmaxf(mn, ml[u].x);
+        }
         const float ref = mn == -INFINITY ? 0.f : mn, corr = __builtin_amdgcn_exp2f(m - ref);
         m = mn;
         l *= corr;
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[i] *= corr;
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
+        for (int u = 0; u < 4; ++u) {
             const float w = __builtin_amdgcn_exp2f(ml[u].x - ref);
             l += ml[u].y * w;
-            if (j + u * kJoinWaves <= j1)
+            if (j + u * kJoinWaves <= j1)      // what is behind them was never written
 #pragma unroll
                 for (int i = 0; i < 4; ++i) acc[i] += x[u][i] * w;
         }

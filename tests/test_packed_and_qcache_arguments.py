@@ -119,9 +119,11 @@ def test_shapes_are_checked_by_the_binding():
     with pytest.raises(ValueError, match="GPU tensor"):
         api.QCache(CFG, *parts)
     c = object.__new__(api.QCache)
-    c.heads, c.head_dim, c.rows, c.tensors = 2, 64, 64, dict(k_codes=parts[0])
-    with pytest.raises(ValueError, match="other heads"):
+    c.heads, c.head_dim, c.rows, c.device = 2, 64, 64, -1
+    with pytest.raises(ValueError, match="GPU tensor"):
         api.pkv_qcache_store(CFG, new(3, 2, 128), new(3, 2, 128), c)
+    with pytest.raises(ValueError, match="other heads"):
+        api._of_cache(CFG, c, -1)
     c.head_dim = 128
     for call in (lambda: api.pkv_qcache_store(CFG, new(3, 2, 128), new(4, 2, 128), c),
                  lambda: api.pkv_qcache_store(CFG, new(3, 2, 128), new(3, 2, 128), c, i32(4)),
