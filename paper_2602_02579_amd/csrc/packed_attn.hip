@@ -7,12 +7,13 @@
 // one, and the tiles are known without a look at the lengths.  It goes over the keys from the first
 // that one of its rows sees to the last, 64 at a time; every column masks with its own two ends, and
 // a wave skips what none of its columns sees.  K and V tiles come into LDS by direct loads, the
-// next one while one is used; 64 KB (head_dim 128) leave room for a second workgroup on the CU, whose
+// next ones while some are used; 64 KB (head_dim 128) leave room for a second workgroup on the CU, whose
 // products run under this one's exponentials.
 //
 // The reference of a column's exponentials follows the running maximum only when that is 2^8 or more
 // above it: most tiles neither rescale nor exchange anything between lanes.
 #include <atomic>
+#include <type_traits>
 
 #include "attn_common.h"
 #include "attn_tile.h"
@@ -20,6 +21,18 @@
 namespace pkv {
 
 namespace {
+
+// x is made here: the compiler would move what is used later behind the loop's matrix instructions.
+template <typename V>
+__device__ __forceinline__ void here(V& x) {
+    asm volatile("" : "+v"(x));
+}
+// What is made from x is made where it is used: made in front of the loop, as the compiler would, it
+// takes the place of accumulators.
+template <typename V>
+__device__ __forceinline__ void not_ahead(V& x) {
+    here(x);
+}
 
 template <typename T>
 struct PackedParams {
@@ -106,19 +119,17 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void packed_attn_kerne
 
     // ---- this lane's column ---------------------------------------------------------------------
     const int64_t col = (int64_t)tile * kCols + wave * 32 + l32;
-    const int row = (int)(col / p.group), head = g * p.group + (int)(col - (int64_t)row * p.group);
-    const bool valid = row < p.m;
+    const bool valid = col < (int64_t)p.m * p.group;
     int lo, hi;
-    keys_of(p.row_pos, row, valid, &lo, &hi);
     bf16x8 qreg[KC];
     {
-        const bf16_t* qp = p.q + ((int64_t)row * p.hq + head) * p.D + hh * 8;
+        const int row = (int)(col / p.group), head = g * p.group + (int)(col - (int64_t)row * p.group);
+        keys_of(p.row_pos, row, valid, &lo, &hi);
+        // rows behind the last one: the last one's queries, for nobody
+        const bf16_t* qp = p.q + ((int64_t)min(row, p.m - 1) * p.hq + head) * p.D + hh * 8;
 #pragma unroll
-        for (int kc = 0; kc < KC; ++kc) {
-            bf16x8 z = {};
-            if (valid && kc * 16 + hh * 8 < p.D) z = *reinterpret_cast<const bf16x8*>(qp + kc * 16);
-            qreg[kc] = z;
-        }
+        for (int kc = 0; kc < KC; ++kc)
+            qreg[kc] = kc * 16 + hh * 8 < p.D ? *reinterpret_cast<const bf16x8*>(qp + kc * 16) : bf16x8{};
     }
     // what some column of the wave sees, and what all of them that see anything do
     int w_lo = lo, w_hi = hi, in_lo = hi ? lo : 0, in_hi = hi ? hi : 0x7fffffff;
@@ -147,44 +158,60 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void packed_attn_kerne
     // likewise, for the four rows of a transposing read.
     auto k_swz = [](int r) { return DP == 64 ? (r >> 1) & 7 : r & 15; };
     auto v_swz = [](int r) { return DP == 64 ? 2 * (r & 2) : 4 * (r & 3); };
-    const uint32_t lds = (uint32_t)(uintptr_t)smem;
-    const uint32_t lds_fill = __builtin_amdgcn_readfirstlane(lds + wave * FILLS * 1024);
+    constexpr int RPI = 64 / CH;              // rows of a fill instruction
+    const uint32_t lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)smem);
     const uint32_t row_bytes = (uint32_t)p.hkv * p.D * 2;
-    const int last_piece = p.D / 8 - 1;
-    uint32_t k_off[FILLS], v_off[FILLS];
+    const int fill_row = wave * FILLS * RPI + lane / CH;
+    const uint32_t k_piece = (uint32_t)((lane % CH) ^ k_swz(fill_row)) * 16;
+    const uint32_t v_piece = (uint32_t)((lane % CH) ^ v_swz(fill_row)) * 16;
+    // instruction i takes rows RPI i further, whose swizzle differs by these bits
+    auto k_bits = [](int i) { return (uint32_t)(DP == 64 ? 64 * (i & 1) : 16 * RPI * i); };
+    auto v_bits = [](int i) { return (uint32_t)(DP == 256 ? 128 * (i & 1) : 0); };
+    const unsigned char* const k_head =
+        reinterpret_cast<const unsigned char*>(p.k + ((int64_t)k_lo * p.hkv + g) * p.D);
+    const unsigned char* const v_head =
+        reinterpret_cast<const unsigned char*>(p.v + ((int64_t)k_lo * p.hkv + g) * p.D);
+    // Keys lie in four places for 32 (a half tile), values in two places for 64 behind them.  This wave's
+    // rows of a 64-row fill that begins at `row0`, to lds_dst; head: the head's keys or values
+    auto fill = [&](const unsigned char* head, uint32_t piece, auto bits, uint32_t dst, int row0) {
+        const int last = k_hi - k_lo - 1 - row0;
+        const unsigned char* base = head + (int64_t)row0 * row_bytes;
+        if (last >= kBN - 1 && p.D == DP) {   // (a row is a multiple of kRow: the bits are the piece's)
+            uint32_t off = (uint32_t)fill_row * row_bytes + piece;
+            not_ahead(off);
 #pragma unroll
-    for (int i = 0; i < FILLS; ++i) {
-        const int x = (wave * FILLS + i) * 64 + lane, r = x / CH, c = x % CH;
-        k_off[i] = (uint32_t)min(c ^ k_swz(r), last_piece) * 16;
-        v_off[i] = (uint32_t)min(c ^ v_swz(r), last_piece) * 16;
-    }
-    const bf16_t* const k_head = p.k + ((int64_t)k_lo * p.hkv + g) * p.D;
-    const bf16_t* const v_head = p.v + ((int64_t)k_lo * p.hkv + g) * p.D;
-    auto fill = [&](int t) {
-        const int last = k_hi - k_lo - 1 - t * kBN;    // rows behind the last one repeat it
-        const int64_t base = (int64_t)t * kBN * p.hkv * p.D;
-        const uint32_t dst = lds_fill + (t & 1) * 2 * kTile;
+            for (int i = 0; i < FILLS; ++i)
+                dma16(base + (uint32_t)(i * RPI) * row_bytes, off ^ bits(i), dst + i * 1024);
+        } else if (last >= 0) {               // rows behind the last one repeat it, pieces likewise
+            int row = fill_row;
+            not_ahead(row);
+            not_ahead(piece);
 #pragma unroll
-        for (int i = 0; i < FILLS; ++i) {
-            const int r = min(((wave * FILLS + i) * 64 + lane) / CH, last);
-            dma16(k_head + base, (uint32_t)r * row_bytes + k_off[i], dst + i * 1024);
-            dma16(v_head + base, (uint32_t)r * row_bytes + v_off[i], dst + kTile + i * 1024);
+            for (int i = 0; i < FILLS; ++i)
+                dma16(base, (uint32_t)min(row + i * RPI, last) * row_bytes +
+                                min(piece ^ bits(i), (uint32_t)p.D * 2 - 16), dst + i * 1024);
         }
+    };
+    // key halves u and u + 1: the lower two waves fill the first of them
+    auto fill_k = [&](int u) {
+        const uint32_t dst = lds + ((u + (wave >> 1)) & 3) * (kTile / 2) + (wave & 1) * FILLS * 1024;
+        fill(k_head, k_piece, k_bits, dst, 32 * u);
+    };
+    auto fill_v = [&](int t) {
+        fill(v_head, v_piece, v_bits, lds + (2 + (t & 1)) * kTile + wave * FILLS * 1024, kBN * t);
     };
 
     // ---- LDS -> operands -----------------------------------------------------------------------------
     // A row i of a 32-key block is key swap_bits_2_3(i): a lane's 16 scores are then the keys 8 hh + 0..7
     // and 16 + 8 hh + 0..7, the B operands of the second product
     const int prow = (l32 & 0x13) | ((l32 & 4) << 1) | ((l32 & 8) >> 1);
-    uint32_t kaddr[KC], vaddr[DB];
-#pragma unroll
-    for (int kc = 0; kc < KC; ++kc)
-        kaddr[kc] = (uint32_t)(prow * kRow + (((2 * kc + hh) ^ k_swz(prow)) * 16));
+    const uint32_t kaddr = (uint32_t)(prow * kRow + ((hh ^ k_swz(prow)) * 16));   // ^ 32 kc
+    uint32_t vaddr[DB];
     {
         const int e = (lane >> 2) & 3, j = lane & 3, gh = (lane >> 4) & 1;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
-            vaddr[db] = (uint32_t)(kTile + (8 * hh + e) * kRow +
+            vaddr[db] = (uint32_t)(2 * kTile + (8 * hh + e) * kRow +
                                    ((db * 4 + gh * 2 + (j >> 1)) ^ v_swz(e)) * 16 + (j & 1) * 8);
     }
 
@@ -195,81 +222,158 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void packed_attn_kerne
 #pragma unroll
         for (int r = 0; r < 16; ++r) o_acc[db][r] = 0.f;
 
-    if (n_iter > 0) fill(0);
-    if (n_iter > 1) fill(1);
-    for (int t = 0; t < n_iter; ++t) {
-        if (t + 1 < n_iter) wait_vm<2 * FILLS>();   // this tile has landed, the next is on its way
-        else wait_vm<0>();
-        __syncthreads();
-        const int key0 = k_lo + t * kBN;
-        if (key0 < w_hi && key0 + kBN > w_lo) {
-            const unsigned char* st = smem + (t & 1) * 2 * kTile;
-            f32x16 s[2];
+    // The scores of the next half tile are multiplied while the exponentials of this one are worked out, its
+    // values while the maximum of those scores is found: each matrix instruction has vector instructions
+    // to run beside it.  So keys are half a tile ahead of values.
+    const int first = w_hi > w_lo ? (w_lo - k_lo) / 32 : 0x7fffffff;   // halves first .. last - 1 hold
+    const int last = w_hi > w_lo ? (w_hi - k_lo + 31) / 32 : 0;        // keys that some column sees
+    auto k_op = [&](int u, int kc) __attribute__((always_inline)) {
+        return *reinterpret_cast<const bf16x8*>(smem + (u & 3) * (kTile / 2) + (kaddr ^ 32 * kc));
+    };
+    auto v_op = [&](int u, int i) __attribute__((always_inline)) {   // i: block of elements, then of keys
+        const unsigned char* a = smem + (u >> 1 & 1) * kTile + (u & 1) * 32 * kRow +
+                                 16 * (i / DB) * kRow + vaddr[i % DB];
+        const bf16x4 x = lds_read_tr(a), y = lds_read_tr(a + 4 * kRow);
+        return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    auto largest = [&](const f32x16& s) __attribute__((always_inline)) {
+        float top = s[0];
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+        for (int r = 1; r < 16; ++r) top = fmaxf(top, s[r]);
+        return top;
+    };
+    // the ends of the columns' keys, and the reference; s: of half u, top: its largest
+    auto settle = [&](int u, f32x16& s, float top) __attribute__((always_inline)) {
+        const int key0 = k_lo + 32 * u;
+        if (__builtin_expect(key0 < in_lo || key0 + 32 > in_hi, 0)) {
+            // element r is key 16 (r / 8) + 8 hh + r % 8
+            const int a = lo - key0 - 8 * hh, b = hi - key0 - 8 * hh;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[h][r] = 0.f;
-#pragma unroll
-            for (int kc = 0; kc < KC; ++kc)
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    s[h] = mfma32(*reinterpret_cast<const bf16x8*>(st + h * 32 * kRow + kaddr[kc]),
-                                  qreg[kc], s[h]);
-            if (key0 < in_lo || key0 + kBN > in_hi) {
-                // element r of block h is key 32 h + 16 (r / 8) + 8 hh + r % 8 of the tile
-                const int a = lo - key0 - 8 * hh, b = hi - key0 - 8 * hh;
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int key = 32 * h + 16 * (r / 8) + r % 8;
-                        if (key < a || key >= b) s[h][r] = -INFINITY;
-                    }
+            for (int r = 0; r < 16; ++r) {
+                const int key = 16 * (r / 8) + r % 8;
+                if (key < a || key >= b) s[r] = -INFINITY;
             }
-            float top = s[0][0];
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) top = fmaxf(top, s[h][r]);
-            top *= p.c2;
-            if (__any(top > m2 + 8.f)) {
-                float mx = fmaxf(top, m2);
-                mx = fmaxf(mx, __shfl_xor(mx, 32));
-                const float corr = mx == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m2 - mx);
-                m2 = mx;
-                l_run *= corr;
-#pragma unroll
-                for (int db = 0; db < DB; ++db)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) o_acc[db][r] *= corr;
-            }
-            const float ref = m2 == -INFINITY ? 0.f : m2;
-            bf16x8 pb[2][2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const float e = __builtin_amdgcn_exp2f(fmaf(s[h][r], p.c2, -ref));
-                    l_run += e;
-                    pb[h][r / 8][r % 8] = (bf16_t)e;
-                }
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-                    for (int db = 0; db < DB; ++db) {
-                        const unsigned char* a = st + (32 * h + 16 * kk) * kRow + vaddr[db];
-                        const bf16x4 x = lds_read_tr(a), y = lds_read_tr(a + 4 * kRow);
-                        const bf16x8 va = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
-                        o_acc[db] = mfma32(va, pb[h][kk], o_acc[db]);
-                    }
+            top = largest(s);
         }
-        __syncthreads();                            // everybody is done with this tile
-        if (t + 2 < n_iter) fill(t + 2);
+        top *= p.c2;
+        if (__builtin_expect(__any(top > m2 + 8.f), 0)) {
+            float mx = fmaxf(top, m2);
+            mx = fmaxf(mx, __shfl_xor(mx, 32));
+            const float corr = mx == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m2 - mx);
+            m2 = mx;
+            l_run *= corr;
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o_acc[db][r] *= corr;
+        }
+    };
+    // Half u (its number modulo 4 is a constant), of which s are the scores, and `next`, those of the half
+    // behind it: a product, its share of the vector work, a product.  Operands are requested three
+    // products ahead; a weight is summed and packed one product behind its exponential.  A wave skips
+    // the halves that none of its columns sees.
+    auto half = [&](auto u4, int u, const f32x16& s, f32x16& next) __attribute__((always_inline)) {
+        constexpr int U = decltype(u4)::value, NK = KC, NV = 2 * DB, AHEAD = 3;
+        if (u + 1 < first || u >= last) return;
+        const float ref = m2 == -INFINITY ? 0.f : m2;
+        bf16x8 op[AHEAD], pb[2];
+        f32x16 zero;
+        float e[16];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) zero[r] = 0.f;
+        auto exponential = [&](int r) __attribute__((always_inline)) {
+            e[r] = __builtin_amdgcn_exp2f(fmaf(s[r], p.c2, -ref));
+            here(e[r]);
+        };
+        auto sum = [&](int r) __attribute__((always_inline)) {
+            l_run += e[r];
+            here(l_run);
+            pb[r / 8][r % 8] = (bf16_t)e[r];
+        };
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) op[i] = k_op(U + 1, i);
+#pragma unroll
+        for (int i = 0; i < NK; ++i) {          // with the first eight weights
+            __builtin_amdgcn_sched_barrier(0);
+            next = mfma32(op[i % AHEAD], qreg[i], i ? next : zero);
+            op[i % AHEAD] = i + AHEAD < NK ? k_op(U + 1, i + AHEAD) : v_op(U, i + AHEAD - NK);
+#pragma unroll
+            for (int r = i * 8 / NK; r < (i + 1) * 8 / NK; ++r) {
+                exponential(r);
+                if (r) sum(r - 1);
+            }
+        }
+        sum(7);
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {          // with the other eight, and then the maximum
+            __builtin_amdgcn_sched_barrier(0);
+            o_acc[i % DB] = mfma32(op[(i + NK) % AHEAD], pb[i / DB], o_acc[i % DB]);
+            if (i + AHEAD < NV) op[(i + NK) % AHEAD] = v_op(U, i + AHEAD);
+            if (i < DB) {
+#pragma unroll
+                for (int r = 8 + i * 8 / DB; r < 8 + (i + 1) * 8 / DB; ++r) {
+                    exponential(r);
+                    if (r > 8) sum(r - 1);
+                }
+                if (i == DB - 1) sum(15);
+            } else {
+#pragma unroll
+                for (int r = (i - DB) * 16 / DB; r < (i - DB + 1) * 16 / DB; ++r)
+                    top = fmaxf(top, next[r]);
+                here(top);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        settle(u + 1, next, top);
+    };
+    // tile t begins: its values and the key halves 2 t + 1 and 2 t + 2 are there, everybody is done with
+    // what the next fills replace
+    auto begin_tile = [&](int t) __attribute__((always_inline)) {
+        wait_vm<0>();
+        __syncthreads();
+        if (t + 1 < n_iter) {
+            fill_k(2 * t + 3);
+            fill_v(t + 1);
+        }
+    };
+    f32x16 s0, s1;      // scores of even halves, of odd ones; weights of 0 in front of the first
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s0[r] = s1[r] = -INFINITY;
+    if (n_iter > 0) {
+        if (wave < 2) fill(k_head, k_piece, k_bits, lds + wave * FILLS * 1024, 0);   // half 0
+        fill_k(1);
+        fill_v(0);
+        wait_vm<0>();
+        // the queries have come too, and nothing waits for them inside the loop, behind fills that are
+        // on their way
+#pragma unroll
+        for (int kc = 0; kc < KC; ++kc) here(qreg[kc]);
+        __syncthreads();
+        if (first == 0 && last > 0) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s0[r] = 0.f;
+#pragma unroll
+            for (int kc = 0; kc < KC; ++kc) s0 = mfma32(k_op(0, kc), qreg[kc], s0);
+            settle(0, s0, largest(s0));
+        }
+        for (int t = 0; t < n_iter; t += 2) {
+            begin_tile(t);
+            half(std::integral_constant<int, 0>{}, 2 * t, s0, s1);
+            half(std::integral_constant<int, 1>{}, 2 * t + 1, s1, s0);
+            if (t + 1 == n_iter) break;
+            begin_tile(t + 1);
+            half(std::integral_constant<int, 2>{}, 2 * t + 2, s0, s1);
+            half(std::integral_constant<int, 3>{}, 2 * t + 3, s1, s0);
+        }
     }
 
     // ---- results -----------------------------------------------------------------------------------
+    int at = l32;
+    not_ahead(at);
+    const int64_t out_col = (int64_t)tile * kCols + wave * 32 + at;
+    const int row = (int)(out_col / p.group);
+    const int head = g * p.group + (int)(out_col - (int64_t)row * p.group);
     const float l = l_run + __shfl_xor(l_run, 32);
     const float inv = hi ? 1.f / l : 0.f;
     bool fine = true;
