@@ -17,6 +17,7 @@
 
 #include "attn_common.h"
 #include "attn_tile.h"
+#include "lane_ops.h"
 
 namespace pkv {
 
@@ -93,9 +94,11 @@ __device__ void attend_alone(const PackedParams<T>& p, int row, int h, int g, in
     }
 #pragma unroll
     for (int e = 0; e < E; ++e)
-        if (lane + 64 * e < p.D) p.out[o + lane + 64 * e] = Elem<T>::from_f32(acc[e] / sum);
+        if (lane + 64 * e < p.D)
+            p.out[o + lane + 64 * e] = Elem<T>::from_f32(lo < hi ? acc[e] / sum : 0.f);
     if (lane == 0 && p.lse)
-        p.lse[(int64_t)row * p.hq + h] = (mx + __builtin_amdgcn_logf(sum)) * kLn2;
+        p.lse[(int64_t)row * p.hq + h] =
+            lo < hi ? (mx + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
 }
 
 // DP: head_dim rounded up to 64, 128 or 256.  Elements between are 0 in the queries; in the tiles they
@@ -108,58 +111,26 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void packed_attn_kerne
     constexpr int kRow = DP * 2;              // bytes of a row in LDS
     constexpr int kTile = kBN * kRow;         // 64 keys of K or of V
     constexpr int FILLS = kTile / 1024 / 4;   // instructions of a wave for a tile
+    constexpr int RPI = 64 / CH;              // rows of a fill instruction
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ int s_lo[4], s_hi[4];
 
     const int tid = threadIdx.x, lane = tid & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wave = uniform(tid >> 6);
     const int hh = lane >> 5, l32 = lane & 31;
     const int g = blockIdx.x % p.hkv;
     const int tile = p.n_tiles - 1 - (int)(blockIdx.x / p.hkv);   // later rows see more: first
-
-    // ---- this lane's column ---------------------------------------------------------------------
-    const int64_t col = (int64_t)tile * kCols + wave * 32 + l32;
-    const bool valid = col < (int64_t)p.m * p.group;
-    int lo, hi;
-    bf16x8 qreg[KC];
-    {
-        const int row = (int)(col / p.group), head = g * p.group + (int)(col - (int64_t)row * p.group);
-        keys_of(p.row_pos, row, valid, &lo, &hi);
-        // rows behind the last one: the last one's queries, for nobody
-        const bf16_t* qp = p.q + ((int64_t)min(row, p.m - 1) * p.hq + head) * p.D + hh * 8;
-#pragma unroll
-        for (int kc = 0; kc < KC; ++kc)
-            qreg[kc] = kc * 16 + hh * 8 < p.D ? *reinterpret_cast<const bf16x8*>(qp + kc * 16) : bf16x8{};
-    }
-    // what some column of the wave sees, and what all of them that see anything do
-    int w_lo = lo, w_hi = hi, in_lo = hi ? lo : 0, in_hi = hi ? hi : 0x7fffffff;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        w_lo = min(w_lo, __shfl_xor(w_lo, o));
-        w_hi = max(w_hi, __shfl_xor(w_hi, o));
-        in_lo = max(in_lo, __shfl_xor(in_lo, o));
-        in_hi = min(in_hi, __shfl_xor(in_hi, o));
-    }
-    w_lo = __builtin_amdgcn_readfirstlane(w_lo);
-    w_hi = __builtin_amdgcn_readfirstlane(w_hi);
-    in_lo = __builtin_amdgcn_readfirstlane(in_lo);
-    in_hi = __builtin_amdgcn_readfirstlane(in_hi);
-    if (lane == 0) {
-        s_lo[wave] = w_lo;
-        s_hi[wave] = w_hi;
-    }
-    __syncthreads();
-    const int k_lo = __builtin_amdgcn_readfirstlane(min(min(s_lo[0], s_lo[1]), min(s_lo[2], s_lo[3])));
-    const int k_hi = __builtin_amdgcn_readfirstlane(max(max(s_hi[0], s_hi[1]), max(s_hi[2], s_hi[3])));
-    const int n_iter = k_hi > k_lo ? (k_hi - k_lo + kBN - 1) / kBN : 0;
+    const uint32_t col0 = (uint32_t)tile * kCols, n_cols = (uint32_t)p.m * p.group;
 
     // ---- global -> LDS -----------------------------------------------------------------------------
+    // Keys are counted down from the tile's last row: that end is known before anything is read.  Half
+    // tile u holds keys k_end - 32 (u + 1) .. + 31; tile t of values halves 2 t + 1 and 2 t.
     // Piece c of K row r lies at c ^ swizzle: the rows of one operand read are in different banks.  V
     // likewise, for the four rows of a transposing read.
+    const int k_end = (int)((min(col0 + kCols, n_cols) - 1) / p.group) + 1;
     auto k_swz = [](int r) { return DP == 64 ? (r >> 1) & 7 : r & 15; };
     auto v_swz = [](int r) { return DP == 64 ? 2 * (r & 2) : 4 * (r & 3); };
-    constexpr int RPI = 64 / CH;              // rows of a fill instruction
-    const uint32_t lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)smem);
+    const uint32_t lds = uniform((uint32_t)(uintptr_t)smem);
     const uint32_t row_bytes = (uint32_t)p.hkv * p.D * 2;
     const int fill_row = wave * FILLS * RPI + lane / CH;
     const uint32_t k_piece = (uint32_t)((lane % CH) ^ k_swz(fill_row)) * 16;
@@ -167,39 +138,62 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void packed_attn_kerne
     // instruction i takes rows RPI i further, whose swizzle differs by these bits
     auto k_bits = [](int i) { return (uint32_t)(DP == 64 ? 64 * (i & 1) : 16 * RPI * i); };
     auto v_bits = [](int i) { return (uint32_t)(DP == 256 ? 128 * (i & 1) : 0); };
-    const unsigned char* const k_head =
-        reinterpret_cast<const unsigned char*>(p.k + ((int64_t)k_lo * p.hkv + g) * p.D);
-    const unsigned char* const v_head =
-        reinterpret_cast<const unsigned char*>(p.v + ((int64_t)k_lo * p.hkv + g) * p.D);
+    const unsigned char* const k_head = reinterpret_cast<const unsigned char*>(p.k + (int64_t)g * p.D);
+    const unsigned char* const v_head = reinterpret_cast<const unsigned char*>(p.v + (int64_t)g * p.D);
     // Keys lie in four places for 32 (a half tile), values in two places for 64 behind them.  This wave's
-    // rows of a 64-row fill that begins at `row0`, to lds_dst; head: the head's keys or values
+    // rows of a 64-row fill that begins at key `row0`, to lds_dst; head: the head's keys or values
     auto fill = [&](const unsigned char* head, uint32_t piece, auto bits, uint32_t dst, int row0) {
-        const int last = k_hi - k_lo - 1 - row0;
-        const unsigned char* base = head + (int64_t)row0 * row_bytes;
-        if (last >= kBN - 1 && p.D == DP) {   // (a row is a multiple of kRow: the bits are the piece's)
+        const unsigned char* const base = head + (int64_t)max(row0, 0) * row_bytes;
+        if (row0 >= 0 && p.D == DP) {         // (a row is a multiple of kRow: the bits are the piece's)
             uint32_t off = (uint32_t)fill_row * row_bytes + piece;
             not_ahead(off);
 #pragma unroll
             for (int i = 0; i < FILLS; ++i)
                 dma16(base + (uint32_t)(i * RPI) * row_bytes, off ^ bits(i), dst + i * 1024);
-        } else if (last >= 0) {               // rows behind the last one repeat it, pieces likewise
-            int row = fill_row;
+        } else if (row0 > -kBN) {             // the first row for those in front of it, pieces likewise
+            int row = fill_row + min(row0, 0);
             not_ahead(row);
             not_ahead(piece);
 #pragma unroll
             for (int i = 0; i < FILLS; ++i)
-                dma16(base, (uint32_t)min(row + i * RPI, last) * row_bytes +
+                dma16(base, (uint32_t)max(row + i * RPI, 0) * row_bytes +
                                 min(piece ^ bits(i), (uint32_t)p.D * 2 - 16), dst + i * 1024);
         }
     };
-    // key halves u and u + 1: the lower two waves fill the first of them
+    // key halves u and u + 1, of which the upper two waves fill the first; values of tile t
     auto fill_k = [&](int u) {
-        const uint32_t dst = lds + ((u + (wave >> 1)) & 3) * (kTile / 2) + (wave & 1) * FILLS * 1024;
-        fill(k_head, k_piece, k_bits, dst, 32 * u);
+        const uint32_t dst =
+            lds + ((u + 1 - (wave >> 1)) & 3) * (kTile / 2) + (wave & 1) * FILLS * 1024;
+        fill(k_head, k_piece, k_bits, dst, k_end - 32 * (u + 2));
     };
     auto fill_v = [&](int t) {
-        fill(v_head, v_piece, v_bits, lds + (2 + (t & 1)) * kTile + wave * FILLS * 1024, kBN * t);
+        fill(v_head, v_piece, v_bits, lds + (2 + (t & 1)) * kTile + wave * FILLS * 1024,
+             k_end - kBN * (t + 1));
     };
+    if (wave >= 2) fill(k_head, k_piece, k_bits, lds + (wave & 1) * FILLS * 1024, k_end - kBN);   // half 0
+    fill_k(1);
+    fill_v(0);
+
+    // ---- this lane's column ---------------------------------------------------------------------
+    int lo, hi;
+    bf16x8 qreg[KC];
+    {
+        const uint32_t col = col0 + wave * 32 + l32;
+        const int row = col / (uint32_t)p.group, head = g * p.group + (int)(col - (uint32_t)row * p.group);
+        keys_of(p.row_pos, row, col < n_cols, &lo, &hi);
+        // rows behind the last one: the last one's queries, for nobody
+        const bf16_t* qp = p.q + ((int64_t)min(row, p.m - 1) * p.hq + head) * p.D + hh * 8;
+#pragma unroll
+        for (int kc = 0; kc < KC; ++kc)
+            qreg[kc] = kc * 16 + hh * 8 < p.D ? *reinterpret_cast<const bf16x8*>(qp + kc * 16) : bf16x8{};
+    }
+    // what some column of the wave sees, and what all of them that see anything do
+    const int w_lo = min32(lo), w_hi = max32(hi);
+    const int in_lo = max32(hi ? lo : 0), in_hi = min32(hi ? hi : 0x7fffffff);
+    if (lane == 0) {
+        s_lo[wave] = w_lo;
+        s_hi[wave] = w_hi;
+    }
 
     // ---- LDS -> operands -----------------------------------------------------------------------------
     // A row i of a 32-key block is key swap_bits_2_3(i): a lane's 16 scores are then the keys 8 hh + 0..7
@@ -225,13 +219,13 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void packed_attn_kerne
     // The scores of the next half tile are multiplied while the exponentials of this one are worked out, its
     // values while the maximum of those scores is found: each matrix instruction has vector instructions
     // to run beside it.  So keys are half a tile ahead of values.
-    const int first = w_hi > w_lo ? (w_lo - k_lo) / 32 : 0x7fffffff;   // halves first .. last - 1 hold
-    const int last = w_hi > w_lo ? (w_hi - k_lo + 31) / 32 : 0;        // keys that some column sees
+    const int first = w_hi > w_lo ? (k_end - w_hi) / 32 : 0x7fffffff;    // halves first .. last - 1 hold
+    const int last = w_hi > w_lo ? (k_end - 1 - w_lo) / 32 + 1 : 0;      // keys that some column sees
     auto k_op = [&](int u, int kc) __attribute__((always_inline)) {
         return *reinterpret_cast<const bf16x8*>(smem + (u & 3) * (kTile / 2) + (kaddr ^ 32 * kc));
     };
     auto v_op = [&](int u, int i) __attribute__((always_inline)) {   // i: block of elements, then of keys
-        const unsigned char* a = smem + (u >> 1 & 1) * kTile + (u & 1) * 32 * kRow +
+        const unsigned char* a = smem + (u >> 1 & 1) * kTile + (~u & 1) * 32 * kRow +
                                  16 * (i / DB) * kRow + vaddr[i % DB];
         const bf16x4 x = lds_read_tr(a), y = lds_read_tr(a + 4 * kRow);
         return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
@@ -244,7 +238,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void packed_attn_kerne
     };
     // the ends of the columns' keys, and the reference; s: of half u, top: its largest
     auto settle = [&](int u, f32x16& s, float top) __attribute__((always_inline)) {
-        const int key0 = k_lo + 32 * u;
+        const int key0 = k_end - 32 * (u + 1);
         if (__builtin_expect(key0 < in_lo || key0 + 32 > in_hi, 0)) {
             // element r is key 16 (r / 8) + 8 hh + r % 8
             const int a = lo - key0 - 8 * hh, b = hi - key0 - 8 * hh;
@@ -269,14 +263,17 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void packed_attn_kerne
         }
     };
     // Half u (its number modulo 4 is a constant), of which s are the scores, and `next`, those of the half
-    // behind it: a product, its share of the vector work, a product.  Operands are requested three
-    // products ahead; a weight is summed and packed one product behind its exponential.  A wave skips
-    // the halves that none of its columns sees.
+    // behind it: a product, its share of the vector work, a product.  Operands are requested AHEAD
+    // products ahead (LDS answers after some 200 clocks, a product takes 32), those of the next half's
+    // keys too where they are there; a weight is summed and packed one product behind its exponential.
+    // A wave skips the halves that none of its columns sees.
+    constexpr int NK = KC, NV = 2 * DB, AHEAD = DP == 256 ? 4 : DP == 128 ? 6 : 4;
+    bf16x8 op[AHEAD];
     auto half = [&](auto u4, int u, const f32x16& s, f32x16& next) __attribute__((always_inline)) {
-        constexpr int U = decltype(u4)::value, NK = KC, NV = 2 * DB, AHEAD = 3;
+        constexpr int U = decltype(u4)::value;
         if (u + 1 < first || u >= last) return;
         const float ref = m2 == -INFINITY ? 0.f : m2;
-        bf16x8 op[AHEAD], pb[2];
+        bf16x8 pb[2];
         f32x16 zero;
         float e[16];
 #pragma unroll
@@ -290,8 +287,10 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void packed_attn_kerne
             here(l_run);
             pb[r / 8][r % 8] = (bf16_t)e[r];
         };
+        if (U % 2 == 0 || u < first) {          // (else the half before has)
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) op[i] = k_op(U + 1, i);
+            for (int i = 0; i < AHEAD; ++i) op[i] = k_op(U + 1, i);
+        }
 #pragma unroll
         for (int i = 0; i < NK; ++i) {          // with the first eight weights
             __builtin_amdgcn_sched_barrier(0);
@@ -305,11 +304,13 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void packed_attn_kerne
         }
         sum(7);
         float top = -INFINITY;
+        bf16x8 after[AHEAD];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {          // with the other eight, and then the maximum
             __builtin_amdgcn_sched_barrier(0);
             o_acc[i % DB] = mfma32(op[(i + NK) % AHEAD], pb[i / DB], o_acc[i % DB]);
             if (i + AHEAD < NV) op[(i + NK) % AHEAD] = v_op(U, i + AHEAD);
+            else if (U % 2 == 0) after[i + AHEAD - NV] = k_op(U + 2, i + AHEAD - NV);
             if (i < DB) {
 #pragma unroll
                 for (int r = 8 + i * 8 / DB; r < 8 + (i + 1) * 8 / DB; ++r) {
@@ -325,8 +326,23 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void packed_attn_kerne
             }
         }
         __builtin_amdgcn_sched_barrier(0);
+        if (U % 2 == 0) {
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) op[i] = after[i];
+        }
         settle(u + 1, next, top);
     };
+    f32x16 s0, s1;      // scores of even halves, of odd ones; weights of 0 in front of the first
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s0[r] = s1[r] = -INFINITY;
+    wait_vm<0>();
+    // the queries have come too, and nothing waits for them inside the loop, behind fills on their way
+#pragma unroll
+    for (int kc = 0; kc < KC; ++kc) here(qreg[kc]);
+    __syncthreads();
+    const int k_lo = uniform(min(min(s_lo[0], s_lo[1]), min(s_lo[2], s_lo[3])));
+    const int k_hi = uniform(max(max(s_hi[0], s_hi[1]), max(s_hi[2], s_hi[3])));
+    const int n_iter = k_hi > k_lo ? (k_end - k_lo + kBN - 1) / kBN : 0;
     // tile t begins: its values and the key halves 2 t + 1 and 2 t + 2 are there, everybody is done with
     // what the next fills replace
     auto begin_tile = [&](int t) __attribute__((always_inline)) {
@@ -337,20 +353,8 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void packed_attn_kerne
             fill_v(t + 1);
         }
     };
-    f32x16 s0, s1;      // scores of even halves, of odd ones; weights of 0 in front of the first
-#pragma unroll
-    for (int r = 0; r < 16; ++r) s0[r] = s1[r] = -INFINITY;
     if (n_iter > 0) {
-        if (wave < 2) fill(k_head, k_piece, k_bits, lds + wave * FILLS * 1024, 0);   // half 0
-        fill_k(1);
-        fill_v(0);
-        wait_vm<0>();
-        // the queries have come too, and nothing waits for them inside the loop, behind fills that are
-        // on their way
-#pragma unroll
-        for (int kc = 0; kc < KC; ++kc) here(qreg[kc]);
-        __syncthreads();
-        if (first == 0 && last > 0) {
+        if (first == 0) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) s0[r] = 0.f;
 #pragma unroll
@@ -368,44 +372,50 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void packed_attn_kerne
         }
     }
 
-    // ---- results -----------------------------------------------------------------------------------
-    int at = l32;
-    not_ahead(at);
-    const int64_t out_col = (int64_t)tile * kCols + wave * 32 + at;
-    const int row = (int)(out_col / p.group);
-    const int head = g * p.group + (int)(out_col - (int64_t)row * p.group);
+    // ---- results: through LDS, so that a column goes out in one piece ------------------------------------
     const float l = l_run + __shfl_xor(l_run, 32);
     const float inv = hi ? 1.f / l : 0.f;
-    bool fine = true;
+    float check = 0.f;                         // 0 as long as all are finite
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-            o_acc[db][r] = hi ? o_acc[db][r] * inv : 0.f;
-            fine = fine && fabsf(o_acc[db][r]) < INFINITY;
+            o_acc[db][r] *= inv;
+            check = fmaf(o_acc[db][r], 0.f, check);
         }
-    fine = fine && (hi == 0 || l < INFINITY);
-    const uint64_t not_fine = __ballot(!fine && valid);
+    int at = l32;
+    not_ahead(at);
+    const uint32_t col = col0 + wave * 32 + at;
+    const int row = col / (uint32_t)p.group, head = g * p.group + (int)(col - (uint32_t)row * p.group);
+    const uint64_t not_fine = __ballot(check != 0.f && col < n_cols);
     const uint32_t alone = (uint32_t)(not_fine | not_fine >> 32);   // by column
-    if (valid && !(alone >> l32 & 1)) {
-        const int64_t oc = (int64_t)row * p.hq + head;
-        bf16_t* op = p.out + oc * p.D + 4 * hh;
+    const bool mine = col < n_cols && !(alone >> at & 1);
+    const int oc = mine ? row * p.hq + head : -1;
+    wait_vm<0>();                              // (tiles without keys: of the first fills)
+    __syncthreads();
+    unsigned char* const so = smem + wave * 32 * kRow;
 #pragma unroll
-        for (int db = 0; db < DB; ++db)
+    for (int db = 0; db < DB; ++db)
 #pragma unroll
-            for (int r4 = 0; r4 < 4; ++r4) {
-                bf16x4 x;
+        for (int r4 = 0; r4 < 4; ++r4) {
+            bf16x4 x;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] = (bf16_t)o_acc[db][4 * r4 + e];
-                if (db * 32 + r4 * 8 + 4 * hh < p.D)
-                    *reinterpret_cast<bf16x4*>(op + db * 32 + r4 * 8) = x;
-            }
-        if (hh == 0 && p.lse)
-            p.lse[oc] = hi ? (m2 + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+            for (int e = 0; e < 4; ++e) x[e] = (bf16_t)o_acc[db][4 * r4 + e];
+            *reinterpret_cast<bf16x4*>(so + at * kRow + ((db * 4 + r4) ^ k_swz(at)) * 16 + hh * 8) = x;
+        }
+    if (hh == 0 && mine && p.lse)
+        p.lse[oc] = hi ? (m2 + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+#pragma unroll
+    for (int i = 0; i < CH / 2; ++i) {
+        const int c = i * RPI + lane / CH, piece = lane % CH;
+        const int to = __shfl(oc, c);
+        if (to >= 0 && piece * 8 < p.D)
+            *reinterpret_cast<bf16x8*>(p.out + (int64_t)to * p.D + piece * 8) =
+                *reinterpret_cast<const bf16x8*>(so + c * kRow + (piece ^ k_swz(c)) * 16);
     }
     for (uint32_t left = alone; left; left &= left - 1) {
-        const int at = __builtin_ctz(left);
-        attend_alone<bf16_t, DP>(p, __shfl(row, at), __shfl(head, at), g, __shfl(lo, at), __shfl(hi, at));
+        const int c = __builtin_ctz(left);
+        attend_alone<bf16_t, DP>(p, __shfl(row, c), __shfl(head, c), g, __shfl(lo, c), __shfl(hi, c));
     }
 }
 
@@ -430,19 +440,12 @@ __global__ __launch_bounds__(NW * 64) void packed_attn_f32_kernel(PackedParams<f
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int g4 = lane >> 4, l16 = lane & 15;
     const int g = blockIdx.y, D = WIDE ? DP : p.D, C = D / 16;
-    const int64_t col = (int64_t)(gridDim.x - 1 - blockIdx.x) * 16 + l16;   // later rows first
-    const int row = (int)(col / p.group), head = g * p.group + (int)(col - (int64_t)row * p.group);
+    const uint32_t col = (gridDim.x - 1 - blockIdx.x) * 16 + l16;   // later rows first
+    const int row = col / (uint32_t)p.group, head = g * p.group + (int)(col - (uint32_t)row * p.group);
     const bool valid = row < p.m;
     int lo, hi;
     keys_of(p.row_pos, row, valid, &lo, &hi);
-    int k_lo = lo, k_hi = hi;
-#pragma unroll
-    for (int o = 8; o > 0; o >>= 1) {
-        k_lo = min(k_lo, __shfl_xor(k_lo, o));
-        k_hi = max(k_hi, __shfl_xor(k_hi, o));
-    }
-    k_lo = __builtin_amdgcn_readfirstlane(k_lo);
-    k_hi = __builtin_amdgcn_readfirstlane(k_hi);
+    const int k_lo = uniform(min16(lo)), k_hi = uniform(max16(hi));
 
     const int64_t krow = (int64_t)p.hkv * D;
     const float* const kb = p.k + (int64_t)g * D + 4 * g4;

@@ -28,6 +28,7 @@
 #include <algorithm>
 #include <atomic>
 
+#include "lane_ops.h"
 #include "qcache.h"
 
 namespace pkv {
@@ -56,21 +57,6 @@ struct QAttnParams {
     int n_wg, log2_wg;            // workgroups of a kv head and column tile, a power of two
     float c2;                     // softmax scale * log2(e)
 };
-
-__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
-
-// v of another lane of the 16 (a rotation), and of lanes in front (0 where there are none)
-template <int CTRL, int ROWS = 0xf>
-__device__ __forceinline__ int dpp(int old, int v) {
-    return __builtin_amdgcn_update_dpp(old, v, CTRL, ROWS, 0xf, false);
-}
-__device__ __forceinline__ int min16(int v) {
-    v = min(v, dpp<0x128>(v, v));
-    v = min(v, dpp<0x124>(v, v));
-    v = min(v, dpp<0x122>(v, v));
-    return min(v, dpp<0x121>(v, v));
-}
-__device__ __forceinline__ int max16(int v) { return -min16(-v); }
 
 // The cache rows of a sequence from `start` on; row_end: the first one that a row does not see
 __device__ __forceinline__ int start_in_cache(const QAttnParams& p, int start) {
@@ -104,16 +90,6 @@ __device__ __forceinline__ Seq seq_of(const QAttnParams& p, int s) {
     const int start = start_in_cache(p, given);
     return {start, groups_of(start, end_of(p, start, pos))};
 }
-__device__ __forceinline__ int wave_scan(int v) {   // inclusive
-    v += dpp<0x111>(0, v);             // from 1, 2, 4, 8 lanes in front, within 16
-    v += dpp<0x112>(0, v);
-    v += dpp<0x114>(0, v);
-    v += dpp<0x118>(0, v);
-    v += dpp<0x142, 0xa>(0, v);        // the last of 16 into the next 16, of 32 into the next 32
-    return v + dpp<0x143, 0xc>(0, v);
-}
-__device__ __forceinline__ int last_lane(int v) { return __builtin_amdgcn_readlane(v, 63); }
-
 // Several sequences: a workgroup's piece of the line of groups, and the sequence that it is in.
 struct Piece {
     int64_t begin, end, before;   // before: groups in front of sequence s
