@@ -28,6 +28,18 @@ __device__ __forceinline__ int min32(int v) {
 }
 __device__ __forceinline__ int max32(int v) { return ~min32(~v); }
 
+// Bits a .. b - 1 of 32, whatever a and b are; x, or -infinity where a bit is not set.  (Comparisons of
+// every element with both ends go through scalar registers: 16 of them took some 800 clocks.)
+__device__ __forceinline__ uint32_t bits_between(int a, int b) {
+    const uint32_t below_b = b >= 32 ? ~0u : (1u << max(b, 0)) - 1u;
+    const uint32_t below_a = a >= 32 ? ~0u : (1u << max(a, 0)) - 1u;
+    return below_b & ~below_a;
+}
+__device__ __forceinline__ float where_bit(uint32_t bits, int at, float x) {
+    const uint32_t on = (uint32_t)__builtin_amdgcn_sbfe((int)bits, at, 1);   // all bits, or none
+    return __uint_as_float((on & __float_as_uint(x)) | (~on & 0xff800000u));
+}
+
 __device__ __forceinline__ int wave_scan(int v) {   // inclusive
     v += dpp<0x111>(0, v);
     v += dpp<0x112>(0, v);

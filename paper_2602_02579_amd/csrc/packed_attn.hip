@@ -49,10 +49,10 @@ constexpr float kLn2 = 0.69314718055994531f;
 constexpr int kCols = 128;     // columns of a workgroup, bf16
 constexpr int kThreads = 256;
 
-// What a row sees: keys lo <= t < hi (nothing: hi == 0)
+// What a row sees: keys lo <= t < hi (nothing: hi == 0, and a lo that stays large minus a few tiles)
 __device__ __forceinline__ void keys_of(const int32_t* row_pos, int row, bool valid, int* lo,
                                         int* hi) {
-    *lo = 0x7fffffff;
+    *lo = 0x7fff0000;
     *hi = 0;
     if (!valid) return;
     const int pos = min(row_pos[row], row);
@@ -241,12 +241,9 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void packed_attn_kerne
         const int key0 = k_end - 32 * (u + 1);
         if (__builtin_expect(key0 < in_lo || key0 + 32 > in_hi, 0)) {
             // element r is key 16 (r / 8) + 8 hh + r % 8
-            const int a = lo - key0 - 8 * hh, b = hi - key0 - 8 * hh;
+            const uint32_t seen = bits_between(lo - key0 - 8 * hh, hi - key0 - 8 * hh);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int key = 16 * (r / 8) + r % 8;
-                if (key < a || key >= b) s[r] = -INFINITY;
-            }
+            for (int r = 0; r < 16; ++r) s[r] = where_bit(seen, 16 * (r / 8) + r % 8, s[r]);
             top = largest(s);
         }
         top *= p.c2;
@@ -509,10 +506,10 @@ __global__ __launch_bounds__(NW * 64) void packed_attn_f32_kernel(PackedParams<f
                 }
         s += s2;
         float top = -INFINITY;
+        const uint32_t seen = bits_between(lo - t - 4 * g4, hi - t - 4 * g4);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int key = t + 4 * g4 + r;
-            s[r] = key >= lo && key < hi ? s[r] * p.c2 : -INFINITY;
+            s[r] = where_bit(seen, r, s[r] * p.c2);
             top = fmaxf(top, s[r]);
         }
         if (__any(top > m2 + 8.f)) {

@@ -379,15 +379,20 @@ __global__ __launch_bounds__(kWaves * 64) void qcache_attn_kernel(QAttnParams p)
                 }
             if (__builtin_expect(edge, 0)) {
 #pragma unroll
-                for (int c = 0; c < NC; ++c)
+                for (int c = 0; c < NC; ++c) {
+                    const uint32_t seen = bits_between(start - key0, end[c] - key0);
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
-                        if (key0 + j < start || key0 + j >= end[c]) sc[c][j >> 2][j & 3] = -INFINITY;
+                        sc[c][j >> 2][j & 3] = where_bit(seen, j, sc[c][j >> 2][j & 3]);
+                }
                 // what no column sees may be any bytes; its weight is 0, and its scales become 1
+                const uint32_t some = bits_between(start - key0, end_max - key0);
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (key0 + j < start || key0 + j >= end_max)
-                        cur.vs[j >> 2] = (cur.vs[j >> 2] & ~(255u << (j & 3) * 8)) | 127u << (j & 3) * 8;
+                for (int j = 0; j < 8; ++j) {
+                    const uint32_t off = ~(uint32_t)__builtin_amdgcn_sbfe((int)some, j, 1) &
+                                         255u << (j & 3) * 8;
+                    cur.vs[j >> 2] = (cur.vs[j >> 2] & ~off) | (off & 0x7f7f7f7fu);
+                }
             }
             bf16x8 pb[NC][PARTS];
 #pragma unroll
