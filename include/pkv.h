@@ -655,6 +655,15 @@ typedef struct {
 
 pkv_status pkv_layer_rows(const pkv_layer_cfg* cfg, const pkv_layer_call* call, void* stream);
 
+/*
+ * The same layer over a packed prompt: the m rows are all of the caches (m == n_cache), dst_row[i] ==
+ * i, and attend as pkv_packed_attn says, row_pos counting inside their sequences.  chunk_len must
+ * be 0 and score NULL (PKV_ERR_SHAPE otherwise).  Scratch: as for pkv_layer_rows, with
+ * pkv_packed_attn_workspace_bytes for the attention.
+ */
+pkv_status pkv_layer_rows_packed(const pkv_layer_cfg* cfg, const pkv_layer_call* call,
+                                 void* stream);
+
 /* Static, never-NULL description of a status code. */
 const char* pkv_status_string(pkv_status status);
 

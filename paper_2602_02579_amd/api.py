@@ -29,7 +29,7 @@ __all__ = ["LayerCfg", "PkvError", "load_library", "library_path",
            "pkv_packed_attn_workspace_bytes", "QCache", "pkv_qcache_store", "pkv_qcache_restore",
            "pkv_qcache_attn", "pkv_qcache_attn_workspace_bytes",
            "pkv_rmsnorm_rows", "pkv_gather_rows", "pkv_linear_rows", "pkv_swiglu_rows",
-           "LayerCall", "pkv_layer_rows", "pkv_glue_workspace_bytes",
+           "LayerCall", "pkv_layer_rows", "pkv_layer_rows_packed", "pkv_glue_workspace_bytes",
            "pkv_workspace_bytes", "pkv_status_string", "pkv_version",
            "EXPORTED_SYMBOLS"]
 
@@ -49,6 +49,7 @@ EXPORTED_SYMBOLS = [
     "pkv_sparse_row_attn_kernel", "pkv_workspace_bytes", "pkv_status_string", "pkv_version",
     "pkv_packed_attn", "pkv_packed_attn_workspace_bytes", "pkv_qcache_store",
     "pkv_qcache_restore", "pkv_qcache_attn", "pkv_qcache_attn_workspace_bytes",
+    "pkv_layer_rows_packed",
 ]
 
 
@@ -173,6 +174,7 @@ def load_library() -> ctypes.CDLL:
                                    ctypes.c_size_t, vp]
     lib.pkv_rope_restore_layers.argtypes = [cfgp, vp, vp, ctypes.c_int32, i32p, i64, i64, vp]
     lib.pkv_layer_rows.argtypes = [cfgp, ctypes.POINTER(LayerCall), vp]
+    lib.pkv_layer_rows_packed.argtypes = [cfgp, ctypes.POINTER(LayerCall), vp]
     lib.pkv_sparse_row_attn_kernel.argtypes = [cfgp, i64, i64]
     lib.pkv_sparse_row_attn_kernel.restype = ctypes.c_int32
     lib.pkv_chunk_attn_workspace_bytes.argtypes = [cfgp, i64, i64]
@@ -202,7 +204,7 @@ def load_library() -> ctypes.CDLL:
                  "pkv_gather_qkv_proj", "pkv_gather_qkv_proj_ex",
                  "pkv_gather_qkv_proj_scatter", "pkv_scatter_kv",
                  "pkv_sparse_row_attn", "pkv_chunk_attn", "pkv_rmsnorm_rows", "pkv_gather_rows",
-                 "pkv_linear_rows", "pkv_swiglu_rows", "pkv_layer_rows",
+                 "pkv_linear_rows", "pkv_swiglu_rows", "pkv_layer_rows", "pkv_layer_rows_packed",
                  "pkv_rope_restore_layers", "pkv_packed_attn", "pkv_qcache_store",
                  "pkv_qcache_restore", "pkv_qcache_attn"):
         getattr(lib, name).restype = ctypes.c_int
@@ -809,7 +811,7 @@ def pkv_layer_rows(cfg: LayerCfg, h: torch.Tensor, x: torch.Tensor, q: torch.Ten
                    score: Optional[torch.Tensor] = None,
                    lse_ctx: Optional[torch.Tensor] = None, n_ctx: int = 0,
                    accumulate: bool = False, chunk_len: int = 0,
-                   stop: int = LAYER_WHOLE) -> None:
+                   stop: int = LAYER_WHOLE, call: str = "pkv_layer_rows") -> None:
     """One decoder layer for the first ``m`` rows of the buffers ``h, x, q, attn, g``.
     ``weights`` maps the nine weight names to tensors, and the names ``variant`` of block variants
     that it also holds."""
@@ -851,4 +853,10 @@ def pkv_layer_rows(cfg: LayerCfg, h: torch.Tensor, x: torch.Tensor, q: torch.Ten
     c.ws, c.ws_bytes = _ws(ws)
     c.m, c.n_cache, c.n_ctx, c.inter, c.chunk_len = m, n_cache, n_ctx, inter, chunk_len
     c.eps, c.accumulate, c.stop = eps, bool(accumulate), stop
-    _check("pkv_layer_rows", load_library().pkv_layer_rows(cfg._ref, ctypes.byref(c), _stream()))
+    _check(call, getattr(load_library(), call)(cfg._ref, ctypes.byref(c), _stream()))
+
+
+def pkv_layer_rows_packed(*args, **kw) -> None:
+    """``pkv_layer_rows`` over a packed prompt: ``row_pos`` counts inside the sequences, and the rows
+    attend as ``pkv_packed_attn`` says."""
+    pkv_layer_rows(*args, call="pkv_layer_rows_packed", **kw)

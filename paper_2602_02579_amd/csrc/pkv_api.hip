@@ -440,11 +440,13 @@ pkv_status pkv_swiglu_rows(int32_t dtype, const void* x, const void* w_gate, con
                           ws_bytes, stream);
 }
 
-pkv_status pkv_layer_rows(const pkv_layer_cfg* cfg, const pkv_layer_call* call, void* stream) {
+static pkv_status layer_rows(const pkv_layer_cfg* cfg, const pkv_layer_call* call, bool packed,
+                             void* stream) {
     pkv_status st = check_cfg(cfg);
     if (st != PKV_OK) return st;
     if (!call) return PKV_ERR_NULL;
     const pkv_layer_call& c = *call;
+    if (packed && (c.chunk_len || c.score || c.m != c.n_cache)) return PKV_ERR_SHAPE;
     if (c.stop < PKV_LAYER_WHOLE || c.stop > PKV_LAYER_TO_CACHES || c.chunk_len < 0)
         return PKV_ERR_SHAPE;
     if (c.chunk_len && (c.score || c.m != c.n_cache)) return PKV_ERR_SHAPE;
@@ -475,7 +477,10 @@ pkv_status pkv_layer_rows(const pkv_layer_cfg* cfg, const pkv_layer_call* call, 
                                      c.ws_bytes, stream, angles));
     }
     if (c.stop == PKV_LAYER_TO_CACHES) return PKV_OK;
-    if (c.chunk_len) {
+    if (packed) {
+        PKV_TRY(pkv_packed_attn(cfg, c.q, c.k_cache, c.v_cache, c.row_pos, c.attn, nullptr, c.m,
+                                0.f, c.ws, c.ws_bytes, stream));
+    } else if (c.chunk_len) {
         PKV_TRY(pkv_chunk_attn(cfg, c.q, c.k_cache, c.v_cache, c.row_pos, c.attn, c.m,
                                c.chunk_len, 0.f, c.ws, c.ws_bytes, stream));
     } else if (c.score && c.lse_ctx) {
@@ -507,6 +512,15 @@ pkv_status pkv_layer_rows(const pkv_layer_cfg* cfg, const pkv_layer_call* call, 
                             stream));
 #undef PKV_TRY
     return PKV_OK;
+}
+
+pkv_status pkv_layer_rows(const pkv_layer_cfg* cfg, const pkv_layer_call* call, void* stream) {
+    return layer_rows(cfg, call, false, stream);
+}
+
+pkv_status pkv_layer_rows_packed(const pkv_layer_cfg* cfg, const pkv_layer_call* call,
+                                 void* stream) {
+    return layer_rows(cfg, call, true, stream);
 }
 
 size_t pkv_glue_workspace_bytes(int32_t dtype, int64_t m, int64_t k_in, int64_t n_out) {

@@ -20,7 +20,8 @@ downloaded index lists.
 
 from __future__ import annotations
 
-from typing import Dict, List, Optional, Sequence, Tuple
+import operator
+from typing import Dict, List, Optional, Sequence, Tuple, Union
 
 import numpy as np
 import torch
@@ -111,9 +112,16 @@ class Diagnostics:
     # every one of their T rows is written before anything reads it, and the inverse rotation runs
     # in place
     def _prefill_into(self, embed_rows: torch.Tensor, blocks: Sequence[Block],
-                      k: List[torch.Tensor], v: List[torch.Tensor], chunk_len: int) -> None:
+                      k: List[torch.Tensor], v: List[torch.Tensor],
+                      chunk_len: Union[int, Sequence[int]]) -> None:
         t = embed_rows.shape[0]
         cr = self._prefill_rows(t)
+        if not isinstance(chunk_len, int):
+            pos = torch.cat([torch.arange(n, dtype=torch.int32) for n in chunk_len]).to(self.device)
+            self._through_layers(cr, embed_rows, blocks, k, v, (
+                cr.h[:t], cr.rows[:t], pos, -pos,
+                api.pkv_packed_attn_workspace_bytes(self.lc, t)), None)
+            return
         if (t, chunk_len) not in cr.views:
             if len(cr.views) == 64:   # views are cheap to make again
                 cr.views.clear()
@@ -125,7 +133,11 @@ class Diagnostics:
             cr.views[t, chunk_len] = (
                 cr.h[:t], cr.rows[:t], pos[:t], neg_pos[:t],
                 api.pkv_chunk_attn_workspace_bytes(self.lc, t, chunk_len))
-        h, rows, pos, neg_pos, need = cr.views[t, chunk_len]
+        self._through_layers(cr, embed_rows, blocks, k, v, cr.views[t, chunk_len], chunk_len)
+
+    def _through_layers(self, cr: CarriedRows, embed_rows, blocks, k, v, views, chunk_len) -> None:
+        h, rows, pos, neg_pos, need = views
+        t = h.shape[0]
         # the layers' scratch is largest with all rows of the set; the attention's depends on the
         # chunks and may be more
         ws = cr.ws if need <= cr.ws.numel() else torch.empty(need, dtype=torch.uint8,
@@ -139,9 +151,15 @@ class Diagnostics:
         api.pkv_rope_restore_layers(self.lc, k, k, neg_pos)   # inverse rotation
 
     def chunk_isolated_cache(self, embed: torch.Tensor, blocks: Sequence[Block],
-                             chunk_len: int):
-        """Per-layer ``(k_nope, v) [n_ctx, Hkv, D]`` with every chunk prefilled alone."""
+                             chunk_len: Union[int, Sequence[int]]):
+        """Per-layer ``(k_nope, v) [n_ctx, Hkv, D]`` with every chunk prefilled alone: chunks of one
+        length, the last one with what is left, or of the given lengths, which make up the context
+        (paragraphs and whole documents are not cut into equal chunks)."""
         n = self.cfg.n_ctx
+        try:
+            chunk_len = operator.index(chunk_len)
+        except TypeError:
+            return self._chunks_of_lengths(embed, blocks, [operator.index(x) for x in chunk_len])
         starts = range(0, n, chunk_len)
         if blocks and not starts:
             raise ValueError(f"no chunks of {chunk_len} tokens in {n}")
@@ -158,6 +176,24 @@ class Diagnostics:
             self._prefill_into(embed[a:b], blocks, [x[a:b] for x in ks], [x[a:b] for x in vs],
                                chunk_len)
         return [x[:end] for x in ks], [x[:end] for x in vs]
+
+    def _chunks_of_lengths(self, embed: torch.Tensor, blocks: Sequence[Block], lens: List[int]):
+        n = self.cfg.n_ctx
+        if any(x <= 0 for x in lens) or sum(lens) != n or embed.shape[0] < n:
+            raise ValueError(f"chunks of positive lengths that make up the {n} rows are needed")
+        shape = (n, self.cfg.n_kv_heads, self.cfg.head_dim)
+        ks, vs = ([torch.empty(shape, dtype=self.dt, device=self.device) for _ in blocks]
+                  for _ in range(2))
+        a = first = 0
+        for i in range(len(lens)):   # groups of whole chunks, up to GROUP_ROWS rows or one chunk
+            group = lens[first:i + 1]
+            if i + 1 == len(lens) or sum(group) + lens[i + 1] > GROUP_ROWS:
+                b = a + sum(group)
+                if blocks:
+                    self._prefill_into(embed[a:b], blocks, [x[a:b] for x in ks],
+                                       [x[a:b] for x in vs], group)
+                a, first = b, i + 1
+        return ks, vs
 
     def full_prefill_cache(self, embed: torch.Tensor, blocks: Sequence[Block]):
         return self.chunk_isolated_cache(embed, blocks, self.cfg.n_ctx)

@@ -12,13 +12,13 @@ Llama block of the models the paper evaluates (Sec. 5.1).
 
 from __future__ import annotations
 
-from typing import Dict, List, Optional
+from typing import Dict, List, Optional, Sequence
 
 import numpy as np
 import torch
 
 from . import api
-from .pipeline import layer_cfg, restore_together
+from .pipeline import layer_cfg, restore_layer, restore_together
 from .synth import Config, select_count
 
 BLOCK_WEIGHTS = ("w_in", "wq", "wk", "wv", "wo", "w_post", "w_gate", "w_up", "w_down")
@@ -96,6 +96,7 @@ class CarriedRows:
     # caches_only: its normalisation and K/V projection, nothing of the rows themselves;
     # scores_only: up to the scores; chunks = (rows of the caches, chunk length): the rows are
     # all of the caches, in chunks that attend within themselves, ``rows`` counting inside them
+    # (a length of None: in chunks of any lengths, which ``rows`` tells)
     def _layer(self, L: Dict[str, torch.Tensor], rows: torch.Tensor, cnt: int,
                score: Optional[bool], caches_only: bool = False,
                scores_only: bool = False, chunks=None,
@@ -104,12 +105,13 @@ class CarriedRows:
         # rows of the key cache, which the query rows' own keys (stored behind the context) do
         # not touch.
         fused = score is not None and self.fuse_stage1 and chunks is None
-        api.pkv_layer_rows(
+        packed = chunks is not None and chunks[1] is None
+        (api.pkv_layer_rows_packed if packed else api.pkv_layer_rows)(
             self.lc, self.h, self.x, self.q, self.attn, self.g, cnt, L, VARIANT_WEIGHTS,
             L["k_cache"], L["v_cache"], rows, rows if chunks is None else chunks[0], self.eps,
             self.ws if ws is None else ws, score=None if score is None else self.score,
             lse_ctx=self.lse_ctx if fused else None, n_ctx=self.n, accumulate=bool(score),
-            chunk_len=0 if chunks is None else chunks[1],
+            chunk_len=0 if chunks is None or packed else chunks[1],
             stop=api.LAYER_TO_CACHES if caches_only else
             api.LAYER_TO_SCORES if scores_only else api.LAYER_WHOLE)
 
@@ -141,7 +143,7 @@ class CarriedRows:
         together = restore_together(self.lc, layers, self.n)
         for li, L in enumerate(layers):
             if not together:
-                api.pkv_rope_restore(self.lc, L["k_nope"], L["k_cache"][:self.n], None, 0)
+                restore_layer(self.lc, L, self.n)
             if li == last and not keep_rows and self._fuse_last:
                 self._layer(L, self.q_rows, self.qn, score=li > 0, scores_only=True)
             elif li == last and not keep_rows:
@@ -164,3 +166,69 @@ class CarriedRows:
     def run(self, embed, layers, n_score_layers: Optional[int] = None) -> torch.Tensor:
         self._stage1(embed, layers, n_score_layers, keep_rows=False)
         return self.stage2(embed, layers)
+
+
+def keep_caches(cfg: Config, keys: Sequence[torch.Tensor], values: Sequence[torch.Tensor],
+                room: int = 0) -> List[api.QCache]:
+    """Every layer's ``keys`` and ``values`` (``[T, Hkv, D]``) in 4 bits, with room for ``room`` rows
+    behind them: of the caches of chunks, what a context is put together from (a layer's ``kept``), and
+    of those that both stages left, what an answer is decoded over (``AnswerRows``)."""
+    lc = layer_cfg(cfg)
+    kept = []
+    for k, v in zip(keys, values):
+        kept.append(api.QCache.empty(lc, k.shape[0] + room, k.device))
+        api.pkv_qcache_store(lc, k, v, kept[-1])
+    return kept
+
+
+class AnswerRows:
+    """Decoding steps over caches in 4 bits: the new rows of ``n_seq`` sequences, ``rows_each`` of each
+    (one, or a few drafted tokens), through every layer.  A layer's keys and values of the rows go into
+    its cache before the rows attend over it.  A step allocates nothing and can be captured."""
+
+    def __init__(self, cfg: Config, inter: int, eps: float, caches: Sequence[api.QCache],
+                 device: torch.device, n_seq: int = 1, rows_each: int = 1):
+        if n_seq < 1 or rows_each < 1:
+            raise ValueError(f"{n_seq} sequences of {rows_each} rows")
+        self.lc, self.eps, self.caches, self.n_seq = layer_cfg(cfg), float(eps), caches, n_seq
+        self.m = m = n_seq * rows_each
+        lc, dt = self.lc, self.lc.torch_dtype
+        hq, hkv, d, hid = lc.n_q_heads, lc.n_kv_heads, lc.head_dim, lc.hidden
+        new = lambda *shape: torch.empty(shape, dtype=dt, device=device)   # noqa: E731
+        self.x, self.g = new(m, hid), new(m, int(inter))
+        self.q, self.attn = new(m, hq, d), new(m, hq, d)
+        self.k, self.v = new(m, hkv, d), new(m, hkv, d)
+        self.dst = torch.empty((n_seq, rows_each), dtype=torch.int32, device=device)
+        self.unused = torch.empty((n_seq, rows_each), dtype=torch.bool, device=device)
+        need = [api.pkv_qcache_attn_workspace_bytes(lc, c.rows, m, n_seq) for c in caches] + [
+            api.pkv_workspace_bytes(api.CALL_GATHER_QKV_PROJ, lc, 0, m),
+            api.pkv_glue_workspace_bytes(dt, m, hq * d, hid),
+            api.pkv_glue_workspace_bytes(dt, m, hid, int(inter)),
+            api.pkv_glue_workspace_bytes(dt, m, int(inter), hid), 256]
+        self.ws = torch.empty(max(need), dtype=torch.uint8, device=device)
+
+    def step(self, h: torch.Tensor, blocks: Sequence[Dict[str, torch.Tensor]], pos: torch.Tensor,
+             start: torch.Tensor) -> torch.Tensor:
+        """``h [m, hid]``: the rows' hidden states, replaced by those behind the last layer.  ``pos``
+        (int32 [m]): their positions in their sequences, in ascending order, negative for a slot that
+        is not used; ``start`` (int32 [n_seq]): the cache rows where the sequences begin, each with
+        room for its new rows."""
+        if len(blocks) != len(self.caches):
+            raise ValueError(f"{len(blocks)} layers, but caches of {len(self.caches)}")
+        lc, ws, m = self.lc, self.ws, self.m
+        in_seq = pos.view(self.dst.shape)
+        torch.add(start.unsqueeze(1), in_seq, out=self.dst)
+        torch.lt(in_seq, 0, out=self.unused)
+        dst = self.dst.masked_fill_(self.unused, -1).view(m)
+        for L, cache in zip(blocks, self.caches):
+            api.pkv_rmsnorm_rows(h, None, L["w_in"], self.eps, self.x)
+            api.pkv_gather_qkv_proj_ex(lc, self.x, None, pos, L["wq"], L["wk"], L["wv"], self.q,
+                                       self.k, self.v, ws=ws, norm_eps=self.eps,
+                                       **{n: L[n] for n in VARIANT_WEIGHTS if n in L})
+            api.pkv_qcache_store(lc, self.k, self.v, cache, dst)
+            api.pkv_qcache_attn(lc, self.q, cache, pos, self.attn, start, self.n_seq, ws=ws)
+            api.pkv_linear_rows(self.attn.view(m, -1), L["wo"], h, h, ws=ws)
+            api.pkv_rmsnorm_rows(h, None, L["w_post"], self.eps, self.x)
+            api.pkv_swiglu_rows(self.x, L["w_gate"], L["w_up"], self.g, ws=ws)
+            api.pkv_linear_rows(self.g, L["w_down"], h, h, ws=ws)
+        return h

@@ -39,11 +39,23 @@ def upload_layer(cfg: Config, layer: Dict[str, np.ndarray],
     return out
 
 
+def restore_layer(lc: api.LayerCfg, L: Dict[str, torch.Tensor], n: int) -> None:
+    """The keys of one layer's context with their positions, into the first ``n`` rows of ``k_cache``.  A
+    layer that holds ``kept``, a cache in 4 bits (``api.QCache``), takes keys and values from there: its
+    first rows, or the rows ``kept_rows`` (int32 [n]) where the context is put together from the chunks
+    of a larger store."""
+    if "kept" in L:
+        api.pkv_qcache_restore(lc, L["kept"], L["k_cache"][:n], L["v_cache"][:n],
+                               L.get("kept_rows"))
+    else:
+        api.pkv_rope_restore(lc, L["k_nope"], L["k_cache"][:n], None, 0)
+
+
 def restore_together(lc: api.LayerCfg, layers: List[Dict[str, torch.Tensor]], n: int) -> bool:
     """Restore the keys of all ``layers`` in one launch, unless some share memory: then the caller
     restores each layer right before it uses it, as it does with a single layer, where the lists
     would only add to the host's time (4 us of a pass of 52)."""
-    if len(layers) == 1:
+    if len(layers) == 1 or any("kept" in L for L in layers):
         return False
     k_in = [L["k_nope"] for L in layers]
     k_out = [L["k_cache"][:n] for L in layers]
@@ -92,7 +104,7 @@ class SelectiveRecompute:
 
     # ---- Stage I ---------------------------------------------------------
     def restore(self, L: Dict[str, torch.Tensor]) -> None:
-        api.pkv_rope_restore(self.lc, L["k_nope"], L["k_cache"][:self.n], None, 0)
+        restore_layer(self.lc, L, self.n)
 
     def score_layer(self, L: Dict[str, torch.Tensor], accumulate: bool) -> None:
         api.pkv_gather_qkv_proj(self.lc, L["hidden"], self.q_rows, self.q_rows,

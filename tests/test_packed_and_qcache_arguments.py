@@ -7,7 +7,7 @@ import os
 import pytest
 import torch
 
-from paper_2602_02579_amd import api
+from paper_2602_02579_amd import api, diagnostics, model, synth
 
 CFG = api.LayerCfg(8, 2, 128, 256, 1e4, "bf16")
 P = 4096          # a pointer that is aligned and never followed
@@ -136,3 +136,44 @@ def test_shapes_are_checked_by_the_binding():
                                              lse_out=torch.zeros(3, 2))):
         with pytest.raises(ValueError, match="must be"):
             call()
+
+
+def test_layer_rows_packed(lib):
+    def status(**over):
+        c = api.LayerCall()
+        c.m = c.n_cache = 4
+        for name, value in over.items():
+            setattr(c, name, value)
+        return lib.pkv_layer_rows_packed(CFG._ref, ctypes.byref(c), None)
+    assert lib.pkv_layer_rows_packed(None, None, None) == 1
+    assert lib.pkv_layer_rows_packed(CFG._ref, None, None) == 1
+    assert status(n_cache=5) == 2 and status(chunk_len=4) == 2 and status(chunk_len=-1) == 2
+    assert status(score=P) == 2 and status(stop=3) == 2
+    assert status() == 1                                       # none of its buffers
+
+
+def test_chunk_lengths_make_up_the_context():
+    cfg = synth.Config("lengths", "bf16", 2, 8, 4, 2, 1, 16, 32, 1e4)
+    dg = diagnostics.Diagnostics(cfg, 32, 1e-5, torch.device("cpu"))
+    embed = torch.zeros((cfg.n_ctx + cfg.n_query, 32), dtype=torch.bfloat16)
+    for lens in ([], [15], [8, 9], [16, 0], [20, -4], (17,)):
+        with pytest.raises(ValueError, match="positive lengths"):
+            dg.chunk_isolated_cache(embed, [], lens)
+    with pytest.raises(ValueError, match="positive lengths"):
+        dg.chunk_isolated_cache(embed[:15], [], [8, 8])
+    for bad in (2.5, [8.0, 8.0], None):
+        with pytest.raises(TypeError):
+            dg.chunk_isolated_cache(embed, [], bad)
+    assert dg.chunk_isolated_cache(embed, [], torch.tensor([7, 9])) == ([], [])
+    assert dg.chunk_isolated_cache(embed, [], [1] * 16) == ([], [])
+
+
+def test_answer_rows_check_their_counts():
+    cfg = synth.Config("answer", "bf16", 2, 8, 4, 2, 1, 16, 32, 1e4)
+    for n_seq, each in ((0, 1), (1, 0), (-1, 1)):
+        with pytest.raises(ValueError):
+            model.AnswerRows(cfg, 32, 1e-5, [], torch.device("cpu"), n_seq, each)
+    rows = model.AnswerRows(cfg, 32, 1e-5, [], torch.device("cpu"), 2)
+    i32 = torch.zeros(2, dtype=torch.int32)
+    with pytest.raises(ValueError, match="layers"):
+        rows.step(torch.zeros((2, 32), dtype=torch.bfloat16), [{}], i32, i32)
