@@ -237,7 +237,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void packed_attn_kerne
         return top;
     };
     // the ends of the columns' keys, and the reference; s: of half u, top: its largest
-    auto settle = [&](int u, f32x16& s, float top) __attribute__((always_inline)) {
+    auto settle = [&](int u, f32x16& s, float top, auto begins) __attribute__((always_inline)) {
         const int key0 = k_end - 32 * (u + 1);
         if (__builtin_expect(key0 < in_lo || key0 + 32 > in_hi, 0)) {
             // element r is key 16 (r / 8) + 8 hh + r % 8
@@ -252,6 +252,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void packed_attn_kerne
             mx = fmaxf(mx, __shfl_xor(mx, 32));
             const float corr = mx == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m2 - mx);
             m2 = mx;
+            if (decltype(begins)::value) return;   // nothing has been added up
             l_run *= corr;
 #pragma unroll
             for (int db = 0; db < DB; ++db)
@@ -327,7 +328,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void packed_attn_kerne
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i) op[i] = after[i];
         }
-        settle(u + 1, next, top);
+        settle(u + 1, next, top, std::false_type{});
     };
     f32x16 s0, s1;      // scores of even halves, of odd ones; weights of 0 in front of the first
 #pragma unroll
@@ -356,7 +357,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void packed_attn_kerne
             for (int r = 0; r < 16; ++r) s0[r] = 0.f;
 #pragma unroll
             for (int kc = 0; kc < KC; ++kc) s0 = mfma32(k_op(0, kc), qreg[kc], s0);
-            settle(0, s0, largest(s0));
+            settle(0, s0, largest(s0), std::true_type{});
         }
         for (int t = 0; t < n_iter; t += 2) {
             begin_tile(t);
@@ -372,14 +373,15 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void packed_attn_kerne
     // ---- results: through LDS, so that a column goes out in one piece ------------------------------------
     const float l = l_run + __shfl_xor(l_run, 32);
     const float inv = hi ? 1.f / l : 0.f;
-    float check = 0.f;                         // 0 as long as all are finite
+    float checks[4] = {0.f, 0.f, 0.f, 0.f};    // 0 as long as all are finite
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             o_acc[db][r] *= inv;
-            check = fmaf(o_acc[db][r], 0.f, check);
+            checks[r % 4] = fmaf(o_acc[db][r], 0.f, checks[r % 4]);
         }
+    const float check = (checks[0] + checks[1]) + (checks[2] + checks[3]);
     int at = l32;
     not_ahead(at);
     const uint32_t col = col0 + wave * 32 + at;
@@ -402,14 +404,18 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void packed_attn_kerne
         }
     if (hh == 0 && mine && p.lse)
         p.lse[oc] = hi ? (m2 + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+    int to[CH / 2];
+    bf16x8 x[CH / 2];
 #pragma unroll
-    for (int i = 0; i < CH / 2; ++i) {
+    for (int i = 0; i < CH / 2; ++i) {         // all requested before the first goes out
         const int c = i * RPI + lane / CH, piece = lane % CH;
-        const int to = __shfl(oc, c);
-        if (to >= 0 && piece * 8 < p.D)
-            *reinterpret_cast<bf16x8*>(p.out + (int64_t)to * p.D + piece * 8) =
-                *reinterpret_cast<const bf16x8*>(so + c * kRow + (piece ^ k_swz(c)) * 16);
+        to[i] = __shfl(oc, c);
+        x[i] = *reinterpret_cast<const bf16x8*>(so + c * kRow + (piece ^ k_swz(c)) * 16);
     }
+#pragma unroll
+    for (int i = 0; i < CH / 2; ++i)
+        if (to[i] >= 0 && lane % CH * 8 < p.D)
+            *reinterpret_cast<bf16x8*>(p.out + (int64_t)to[i] * p.D + lane % CH * 8) = x[i];
     for (uint32_t left = alone; left; left &= left - 1) {
         const int c = __builtin_ctz(left);
         attend_alone<bf16_t, DP>(p, __shfl(row, c), __shfl(head, c), g, __shfl(lo, c), __shfl(hi, c));
