@@ -221,10 +221,14 @@ __global__ __launch_bounds__(kWaves * 64) void qcache_attn_kernel(QAttnParams p)
     for (int f = 0; f < (EXACT ? 1 : F); ++f) {
         const int d = EXACT ? g4 * (DP / 4) : 32 * f + 8 * g4 < D ? 32 * f + 8 * g4 : 0;
         k_off[f] = krow * code_row + d / 2;
-        ks_off[f] = krow * scale_row + d / kQBlock;
+        ks_off[f] = krow * scale_row + (EXACT ? d / kQBlock & ~3 : d / kQBlock);
     }
+    // Scales come by whole words: what makes a number of fewer bits whole would move in front of the
+    // loop's end and wait for the load there.
+    const int ks_shift = EXACT ? (g4 * (DP / 4) / kQBlock & 3) * 8 : 0;
     const int vd = EXACT || l16 * VB < D ? l16 * VB : 0;
-    const int v_off = 8 * g4 * code_row + vd / 2;
+    const int v_off = 8 * g4 * code_row + (vd / 2 & ~3);
+    const int v_shift = DP == 64 ? (vd / 2 & 3) * 8 : 0;
     const int vs_off = (g4 * scale_row + vd / kQBlock) * 8;
     auto load = [&](int r0, Tile<DP>& t) __attribute__((always_inline)) {
         const int64_t row = (int64_t)h * p.rows + r0;   // r0: a multiple of 32 below rows
@@ -244,7 +248,7 @@ __global__ __launch_bounds__(kWaves * 64) void qcache_attn_kernel(QAttnParams p)
                 const auto c = __builtin_amdgcn_raw_buffer_load_b64(kc, k_off[0], c0, 0);
                 t.kc[kt][0] = c[0];
                 t.kc[kt][1] = c[1];
-                t.ks[kt][0] = __builtin_amdgcn_raw_buffer_load_b8(ks, ks_off[0], s0, 0);
+                t.ks[kt][0] = __builtin_amdgcn_raw_buffer_load_b32(ks, ks_off[0], s0, 0);
             } else {
 #pragma unroll
                 for (int x = 0; x < F; x += 4) {
@@ -252,17 +256,12 @@ __global__ __launch_bounds__(kWaves * 64) void qcache_attn_kernel(QAttnParams p)
 #pragma unroll
                     for (int f = 0; f < 4; ++f) t.kc[kt][x + f] = c[f];
                 }
-                if constexpr (DP == 128)
-                    t.ks[kt][0] = __builtin_amdgcn_raw_buffer_load_b16(ks, ks_off[0], s0, 0);
-                else
-                    t.ks[kt][0] = __builtin_amdgcn_raw_buffer_load_b32(ks, ks_off[0], s0, 0);
+                t.ks[kt][0] = __builtin_amdgcn_raw_buffer_load_b32(ks, ks_off[0], s0, 0);
             }
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            if constexpr (DP == 64) {
-                t.vc[j][0] = __builtin_amdgcn_raw_buffer_load_b16(vc, v_off, j * code_row, 0);
-            } else if constexpr (DP == 128) {
+            if constexpr (DP <= 128) {
                 t.vc[j][0] = __builtin_amdgcn_raw_buffer_load_b32(vc, v_off, j * code_row, 0);
             } else {
                 const auto c = __builtin_amdgcn_raw_buffer_load_b64(vc, v_off, j * code_row, 0);
@@ -287,28 +286,48 @@ __global__ __launch_bounds__(kWaves * 64) void qcache_attn_kernel(QAttnParams p)
         const int g = MULTI ? (int)(piece.begin - piece.before) : (int)blockIdx.x;
         const int step = (MULTI ? 1 : p.n_wg) * kGroup;
         int r0 = base + wave * 32 + g * kGroup;
-        Tile<DP> t0, t1, t2;      // whether a row sees them turns out behind the requests
+        // Requests in the order of use: the first tile, the queries, the second tile (whether a row sees
+        // them turns out behind the requests).
+        Tile<DP> t0, t1, t2;
         load(min(r0, p.rows - 32), t0);
-        load(min(r0 + step, p.rows - 32), t1);
 
         // ---- this lane's columns (the last one again behind it): queries and what they see ------
-        int end[NC], end_min, end_max, q_at[NC];
         // the tile's first row, and a lane's row and head as seen from there
         const int row0 = p.each == 1 ? s : s * p.each + tile0 / p.group;
+        int down[NC], q_at[NC];
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int col = min(tile0 + c * 16 + l16, p.cols - 1);
+            const int in_seq = p.each == 1 ? 0 : col / p.group;
+            down[c] = s * p.each + in_seq - row0;
+            q_at[c] = down[c] * p.hq + col - in_seq * p.group;
+        }
+        typedef typename Vec16<T>::type vec_t;
+        constexpr int QV = 8 / Vec16<T>::N;
+        vec_t q_in[NC][F][QV];
+        {
+            const T* const q0 = static_cast<const T*>(p.q) + ((int64_t)row0 * p.hq + h * p.group) * D;
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+#pragma unroll
+                for (int f = 0; f < F; ++f) {
+                    const int d = EXACT ? g4 * (DP / 4) + 8 * f : 32 * f + 8 * g4;
+                    const vec_t* q = reinterpret_cast<const vec_t*>(q0 + (uint32_t)(q_at[c] * D + d));
+#pragma unroll
+                    for (int i = 0; i < QV; ++i) q_in[c][f][i] = EXACT || d < D ? q[i] : vec_t{};
+                }
+        }
+        load(min(r0 + step, p.rows - 32), t1);
+
+        int end[NC], end_min, end_max;
         if (p.each == 1) {
             end_min = end_max = uniform(row_end(p, start, s));
 #pragma unroll
-            for (int c = 0; c < NC; ++c) {
-                end[c] = end_max;
-                q_at[c] = min(tile0 + c * 16 + l16, p.cols - 1);
-            }
+            for (int c = 0; c < NC; ++c) end[c] = end_max;
         } else {
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
-                const int col = min(tile0 + c * 16 + l16, p.cols - 1), in_seq = col / p.group;
-                const int down = s * p.each + in_seq - row0;
-                end[c] = row_end(p, start, row0 + down);
-                q_at[c] = down * p.hq + col - in_seq * p.group;
+                end[c] = row_end(p, start, row0 + down[c]);
                 end_min = c ? min(end_min, end[c]) : end[c];
                 end_max = c ? max(end_max, end[c]) : end[c];
             }
@@ -316,28 +335,18 @@ __global__ __launch_bounds__(kWaves * 64) void qcache_attn_kernel(QAttnParams p)
             end_max = uniform(max16(end_max));
         }
         bf16x8 qf[NC][PARTS][F];
-        {
-            const T* const q0 = static_cast<const T*>(p.q) + ((int64_t)row0 * p.hq + h * p.group) * D;
 #pragma unroll
-            for (int c = 0; c < NC; ++c)
+        for (int c = 0; c < NC; ++c)
 #pragma unroll
-                for (int f = 0; f < F; ++f) {
-                    typedef typename Vec16<T>::type vec_t;
-                    const int d = EXACT ? g4 * (DP / 4) + 8 * f : 32 * f + 8 * g4;
-                    const vec_t* q = reinterpret_cast<const vec_t*>(q0 + (uint32_t)(q_at[c] * D + d));
-                    vec_t x[8 / Vec16<T>::N];
+            for (int f = 0; f < F; ++f)
 #pragma unroll
-                    for (int i = 0; i < 8 / Vec16<T>::N; ++i) x[i] = EXACT || d < D ? q[i] : vec_t{};
+                for (int e = 0; e < 8; ++e) {
+                    bf16_t part[PARTS];
+                    if constexpr (PARTS == 1) part[0] = q_in[c][f][0][e];
+                    else split<PARTS>(q_in[c][f][e / 4][e % 4], part);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        bf16_t part[PARTS];
-                        if constexpr (PARTS == 1) part[0] = x[0][e];
-                        else split<PARTS>(x[e / 4][e % 4], part);
-#pragma unroll
-                        for (int i = 0; i < PARTS; ++i) qf[c][i][f][e] = part[i];
-                    }
+                    for (int i = 0; i < PARTS; ++i) qf[c][i][f][e] = part[i];
                 }
-        }
         // all rows of the sequence have a say in the line's groups, this tile's in the single one's
         const int groups = MULTI ? piece.seq.groups : groups_of(start, end_max);
         const int g_end = MULTI ? (int)min((int64_t)groups, piece.end - piece.before) : groups;
@@ -366,7 +375,7 @@ __global__ __launch_bounds__(kWaves * 64) void qcache_attn_kernel(QAttnParams p)
             for (int f = 0; f < F; ++f)
 #pragma unroll
                 for (int kt = 0; kt < 2; ++kt) {
-                    const float scale = EXACT ? scale_at(cur.ks[kt][0], f >> 1)
+                    const float scale = EXACT ? scale_at(cur.ks[kt][0] >> ks_shift, f >> 1)
                                               : scale_at(cur.ks[kt][f >> 2], f & 3);
                     u32x4 w;
 #pragma unroll
@@ -453,9 +462,10 @@ __global__ __launch_bounds__(kWaves * 64) void qcache_attn_kernel(QAttnParams p)
                 u32x4 lo, hi;
 #pragma unroll
                 for (int j = 0; j < 8; j += 2) {
-                    const uint32_t x0 = cvt2(cur.vc[j][f >> 3], scale_at(vs[j >> 2], j & 3), (f & 7) / 2);
-                    const uint32_t x1 =
-                        cvt2(cur.vc[j + 1][f >> 3], scale_at(vs[j >> 2], (j & 3) + 1), (f & 7) / 2);
+                    const uint32_t x0 = cvt2(cur.vc[j][f >> 3] >> v_shift, scale_at(vs[j >> 2], j & 3),
+                                             (f & 7) / 2);
+                    const uint32_t x1 = cvt2(cur.vc[j + 1][f >> 3] >> v_shift,
+                                             scale_at(vs[j >> 2], (j & 3) + 1), (f & 7) / 2);
                     lo[j / 2] = __builtin_amdgcn_perm(x1, x0, 0x05040100u);
                     hi[j / 2] = __builtin_amdgcn_perm(x1, x0, 0x07060302u);
                 }
@@ -472,28 +482,36 @@ __global__ __launch_bounds__(kWaves * 64) void qcache_attn_kernel(QAttnParams p)
 
         // ---- the wave's steps, one or two more on their way -----------------------------------------
         // Behind the last one the loads go on, to rows that are there already: a load that may or may not
-        // have been made would have to be waited for as if it were the one in question.
+        // have been made would have to be waited for as if it were the one in question.  So would one
+        // that some way through the loop leaves out: the loop has a single end.
         auto load_ahead = [&](Tile<DP>& t) __attribute__((always_inline)) {
             const int ahead = r0 + 2 * step;
             load(ahead < r_end ? ahead : r0, t);
         };
-        for (;;) {
-            if (r0 >= r_end) break;
-            if (TWO_AHEAD) load_ahead(t2);
-            use(r0, t0);
-            if (!TWO_AHEAD) load_ahead(t0);
-            r0 += step;
-            if (r0 >= r_end) break;
-            if (TWO_AHEAD) load_ahead(t0);
-            use(r0, t1);
-            if (!TWO_AHEAD) load_ahead(t1);
-            r0 += step;
-            if (!TWO_AHEAD) continue;
-            if (r0 >= r_end) break;
-            load_ahead(t1);
-            use(r0, t2);
-            r0 += step;
+        if constexpr (TWO_AHEAD) {
+            while (r0 + 2 * step < r_end) {
+                load_ahead(t2);
+                use(r0, t0);
+                r0 += step;
+                load_ahead(t0);
+                use(r0, t1);
+                r0 += step;
+                load_ahead(t1);
+                use(r0, t2);
+                r0 += step;
+            }
+        } else {
+            while (r0 + step < r_end) {
+                use(r0, t0);
+                load_ahead(t0);
+                r0 += step;
+                use(r0, t1);
+                load_ahead(t1);
+                r0 += step;
+            }
         }
+        if (r0 < r_end) use(r0, t0);
+        if (TWO_AHEAD && r0 + step < r_end) use(r0 + step, t1);
 
         // ---- the waves meet: 16 columns at a time through LDS, a wave per column, always in the same order
 #pragma unroll
