@@ -90,10 +90,13 @@ __device__ __forceinline__ Seq seq_of(const QAttnParams& p, int s) {
     const int start = start_in_cache(p, given);
     return {start, groups_of(start, end_of(p, start, pos))};
 }
-// Several sequences: a workgroup's piece of the line of groups, and the sequence that it is in.
+// Several sequences: a workgroup's piece of the line of groups, and the sequence that it is in.  To begin
+// a sequence takes a workgroup as long as kBegin groups (its queries and first keys are on their way, its
+// waves have met), and so long is a sequence's place on the line: even pieces take even times.
+constexpr int kBegin = 3;
 struct Piece {
-    int64_t begin, end, before;   // before: groups in front of sequence s
-    int s;
+    int64_t begin, end, before;   // before: of the line, in front of the groups of sequence s
+    int s, extra;                 // extra: what the line has in front of a sequence
     Seq seq;                      // of sequence s
     Seq of_lane;                  // up to 64 sequences: of the one of the lane's number
 };
@@ -104,21 +107,23 @@ __device__ __forceinline__ Piece piece_of(const QAttnParams& p, int j) {
     const int lane = threadIdx.x & 63;
     Piece w = {};
     int64_t total = 0;
-    int incl = 0;
+    int incl = 0, some = 0;       // some: sequences that have groups
     for (int s0 = 0; s0 < p.n_seq; s0 += 64) {
         w.of_lane = lane_seq(p, s0 + lane);
         incl = wave_scan(w.of_lane.groups);
         total += last_lane(incl);
+        some += __popcll(__ballot(w.of_lane.groups > 0));
     }
     // few groups: one each
-    w.begin = total < p.n_wg ? j : (j * total) >> p.log2_wg;
-    w.end = total < p.n_wg ? min(total, (int64_t)j + 1) : ((j + 1) * total) >> p.log2_wg;
+    const bool few = total < p.n_wg;
+    w.extra = few ? 0 : kBegin;
+    total += (int64_t)some * w.extra;
+    w.begin = few ? j : (j * total) >> p.log2_wg;
+    w.end = few ? min(total, (int64_t)j + 1) : ((j + 1) * total) >> p.log2_wg;
     if (w.begin >= w.end) return w;
     for (int s0 = 0; s0 < p.n_seq; s0 += 64) {
-        if (p.n_seq > 64) {
-            w.of_lane = lane_seq(p, s0 + lane);
-            incl = wave_scan(w.of_lane.groups);
-        }
+        if (p.n_seq > 64) w.of_lane = lane_seq(p, s0 + lane);
+        incl = wave_scan(w.of_lane.groups + (w.of_lane.groups > 0 ? w.extra : 0));
         const uint64_t past = __ballot(w.before + incl > w.begin);
         if (past) {
             const int at = __builtin_ctzll(past);
@@ -130,12 +135,12 @@ __device__ __forceinline__ Piece piece_of(const QAttnParams& p, int j) {
         }
         w.before += last_lane(incl);
     }
-    w.end = w.begin;   // not reached: the group is on the line
+    w.end = w.begin;   // not reached: the place is on the line
     return w;
 }
 // The next sequence that has groups; false: there is none
 __device__ __forceinline__ bool next_sequence(const QAttnParams& p, Piece& w) {
-    w.before += w.seq.groups;
+    w.before += w.seq.groups + w.extra;
     while (++w.s < p.n_seq) {
         if (p.n_seq <= 64) {
             w.seq.start = __builtin_amdgcn_readlane(w.of_lane.start, w.s);
@@ -203,6 +208,7 @@ __global__ __launch_bounds__(kWaves * 64) void qcache_attn_kernel(QAttnParams p)
     constexpr int F = DP / 32;                     // contraction steps of a score
     constexpr int VB = DP / 16;                    // output blocks: row i of block f is element VB i + f
     constexpr bool TWO_AHEAD = DP * NC <= 128;     // where the registers hold three tiles
+    constexpr bool NEXT_AHEAD = DP * PARTS < 768;  // and two tiles and queries beside the results
     constexpr int kORow = DP + 4;                  // floats of a column's output in LDS
     extern __shared__ __align__(16) float s_o[];   // [kWaves][16][kORow]
     __shared__ float2 s_ml[kWaves][16];
@@ -279,46 +285,45 @@ __global__ __launch_bounds__(kWaves * 64) void qcache_attn_kernel(QAttnParams p)
         piece = piece_of(p, blockIdx.x);
         if (piece.begin >= piece.end) return;
     }
-    for (;;) {
-        const int s = piece.s;
-        const int start = MULTI ? piece.seq.start : uniform(p.seq_start ? start_in_cache(p, *p.seq_start) : 0);
-        const int base = start & ~31;
-        const int g = MULTI ? (int)(piece.begin - piece.before) : (int)blockIdx.x;
-        const int step = (MULTI ? 1 : p.n_wg) * kGroup;
-        int r0 = base + wave * 32 + g * kGroup;
-        // Requests in the order of use: the first tile, the queries, the second tile (whether a row sees
-        // them turns out behind the requests).
-        Tile<DP> t0, t1, t2;
+    auto first_group = [&]() __attribute__((always_inline)) {
+        return MULTI ? (int)max(piece.begin - piece.before, (int64_t)0) : (int)blockIdx.x;
+    };
+    if (MULTI && piece.before + first_group() >= piece.end) return;   // it ends in front of the groups
+    // Requests in the order of use: the first tile, the queries, the second tile (whether a row sees them
+    // turns out behind the requests).
+    typedef typename Vec16<T>::type vec_t;
+    constexpr int QV = 8 / Vec16<T>::N;
+    const int step = (MULTI ? 1 : p.n_wg) * kGroup;
+    int s, start, r0, row0, down[NC];   // row0: the tile's first row; a lane's rows as seen from there
+    Tile<DP> t0, t1, t2;
+    vec_t q_in[NC][F][QV];
+    auto request = [&]() __attribute__((always_inline)) {
+        s = piece.s;
+        start = MULTI ? piece.seq.start : uniform(p.seq_start ? start_in_cache(p, *p.seq_start) : 0);
+        r0 = (start & ~31) + wave * 32 + first_group() * kGroup;
         load(min(r0, p.rows - 32), t0);
-
-        // ---- this lane's columns (the last one again behind it): queries and what they see ------
-        // the tile's first row, and a lane's row and head as seen from there
-        const int row0 = p.each == 1 ? s : s * p.each + tile0 / p.group;
-        int down[NC], q_at[NC];
+        row0 = p.each == 1 ? s : s * p.each + tile0 / p.group;
+        const T* const q0 = static_cast<const T*>(p.q) + ((int64_t)row0 * p.hq + h * p.group) * D;
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
+            // this lane's columns (the last one again behind it)
             const int col = min(tile0 + c * 16 + l16, p.cols - 1);
             const int in_seq = p.each == 1 ? 0 : col / p.group;
             down[c] = s * p.each + in_seq - row0;
-            q_at[c] = down[c] * p.hq + col - in_seq * p.group;
-        }
-        typedef typename Vec16<T>::type vec_t;
-        constexpr int QV = 8 / Vec16<T>::N;
-        vec_t q_in[NC][F][QV];
-        {
-            const T* const q0 = static_cast<const T*>(p.q) + ((int64_t)row0 * p.hq + h * p.group) * D;
+            const int q_at = down[c] * p.hq + col - in_seq * p.group;
 #pragma unroll
-            for (int c = 0; c < NC; ++c)
+            for (int f = 0; f < F; ++f) {
+                const int d = EXACT ? g4 * (DP / 4) + 8 * f : 32 * f + 8 * g4;
+                const vec_t* q = reinterpret_cast<const vec_t*>(q0 + (uint32_t)(q_at * D + d));
 #pragma unroll
-                for (int f = 0; f < F; ++f) {
-                    const int d = EXACT ? g4 * (DP / 4) + 8 * f : 32 * f + 8 * g4;
-                    const vec_t* q = reinterpret_cast<const vec_t*>(q0 + (uint32_t)(q_at[c] * D + d));
-#pragma unroll
-                    for (int i = 0; i < QV; ++i) q_in[c][f][i] = EXACT || d < D ? q[i] : vec_t{};
-                }
+                for (int i = 0; i < QV; ++i) q_in[c][f][i] = EXACT || d < D ? q[i] : vec_t{};
+            }
         }
         load(min(r0 + step, p.rows - 32), t1);
-
+    };
+    request();
+    for (;;) {
+        const int g = first_group();
         int end[NC], end_min, end_max;
         if (p.each == 1) {
             end_min = end_max = uniform(row_end(p, start, s));
@@ -352,7 +357,7 @@ __global__ __launch_bounds__(kWaves * 64) void qcache_attn_kernel(QAttnParams p)
         const int g_end = MULTI ? (int)min((int64_t)groups, piece.end - piece.before) : groups;
         if (!MULTI && g > 0 && g >= groups) return;
         const bool whole = MULTI ? g == 0 && g_end == groups : p.n_wg == 1;
-        const int r_end = min(end_max, base + g_end * kGroup);
+        const int r_end = min(end_max, (start & ~31) + g_end * kGroup);
 
         float m2[NC], l[NC];
         f32x4 o[NC][VB];
@@ -513,6 +518,19 @@ __global__ __launch_bounds__(kWaves * 64) void qcache_attn_kernel(QAttnParams p)
         if (r0 < r_end) use(r0, t0);
         if (TWO_AHEAD && r0 + step < r_end) use(r0 + step, t1);
 
+        // the next sequence is on its way while the waves meet
+        const int s_now = s;
+        bool more = false;
+        if constexpr (MULTI) {
+            if (blockIdx.y == 0 && blockIdx.z == 0 && threadIdx.x == 0) {
+                if (g == 0) p.held_by[s].x = blockIdx.x;
+                if (g_end == groups) p.held_by[s].y = blockIdx.x;
+            }
+            piece.begin = piece.before + g_end;
+            more = piece.begin < piece.end && next_sequence(p, piece) && piece.before < piece.end;
+            if (more && NEXT_AHEAD) request();
+        }
+
         // ---- the waves meet: 16 columns at a time through LDS, a wave per column, always in the same order
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
@@ -558,7 +576,7 @@ __global__ __launch_bounds__(kWaves * 64) void qcache_attn_kernel(QAttnParams p)
                 }
                 if (whole) {
                     const int in_seq = p.each == 1 ? 0 : col / p.group;
-                    const int64_t oc = (int64_t)(s * p.each + in_seq) * p.hq + h * p.group +
+                    const int64_t oc = (int64_t)(s_now * p.each + in_seq) * p.hq + h * p.group +
                                        (col - in_seq * p.group);
                     const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
@@ -574,7 +592,7 @@ __global__ __launch_bounds__(kWaves * 64) void qcache_attn_kernel(QAttnParams p)
                                                : (m + __builtin_amdgcn_logf(sum)) * kLn2;
                 } else {
                     const int64_t part =
-                        ((int64_t)(MULTI ? blockIdx.x + s : blockIdx.x) * p.hkv + h) * p.cols + col;
+                        ((int64_t)(MULTI ? blockIdx.x + s_now : blockIdx.x) * p.hkv + h) * p.cols + col;
 #pragma unroll
                     for (int i = 0; i < (DP > 128 ? 2 : 1); ++i) {
                         const int d = 2 * lane + 128 * i;
@@ -584,13 +602,8 @@ __global__ __launch_bounds__(kWaves * 64) void qcache_attn_kernel(QAttnParams p)
                 }
             }
         }
-        if constexpr (!MULTI) return;
-        if (blockIdx.y == 0 && blockIdx.z == 0 && threadIdx.x == 0) {
-            if (g == 0) p.held_by[s].x = blockIdx.x;
-            if (g_end == groups) p.held_by[s].y = blockIdx.x;
-        }
-        piece.begin = piece.before + g_end;
-        if (piece.begin >= piece.end || !next_sequence(p, piece)) return;
+        if (!more) return;
+        if (!NEXT_AHEAD) request();
     }
 }
 
