@@ -370,7 +370,8 @@ size_t pkv_chunk_attn_workspace_bytes(const pkv_layer_cfg* cfg, int64_t m, int64
  * are as good.  fp32 softmax and accumulation, one rounding to cfg->dtype.  lse_out, if not NULL,
  * receives the natural-log normaliser per (row, head).  out may be q itself and overlaps no
  * other operand.  softmax_scale == 0 means 1/sqrt(D).  All tensors 16-byte aligned
- * (PKV_ERR_UNSUPPORTED otherwise).  Scratch: pkv_packed_attn_workspace_bytes.  m == 0 is a no-op.
+ * (PKV_ERR_UNSUPPORTED otherwise, where m * Hq > 2^31 - 1, and in fp32 where m * Hq / Hkv >= 2^26).
+ * Scratch: pkv_packed_attn_workspace_bytes.  m == 0 is a no-op.
  */
 pkv_status pkv_packed_attn(const pkv_layer_cfg* cfg,
                            const void* q,          /* [m, Hq, D] */
@@ -450,8 +451,8 @@ pkv_status pkv_qcache_restore(const pkv_layer_cfg* cfg, const pkv_qcache* cache,
  * q, out and lse_out as in pkv_sparse_row_attn (out may be q itself); 16-byte aligned.  fp32
  * softmax and accumulation, one rounding to cfg->dtype.  Meant for few rows a sequence (up to
  * some 64 (row, head of a group) pairs the cache is what is read; beyond, restore it once and use
- * pkv_sparse_row_attn).  n_seq >= 1 divides m.  Deterministic.  Scratch:
- * pkv_qcache_attn_workspace_bytes.  m == 0 is a no-op.
+ * pkv_sparse_row_attn); m * Hq >= 2^23, or 2^20 such pairs of a sequence, is PKV_ERR_UNSUPPORTED.
+ * n_seq >= 1 divides m.  Deterministic.  Scratch: pkv_qcache_attn_workspace_bytes.  m == 0 is a no-op.
  */
 pkv_status pkv_qcache_attn(const pkv_layer_cfg* cfg,
                            const void* q,            /* [m, Hq, D] */

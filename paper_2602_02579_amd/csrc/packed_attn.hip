@@ -12,6 +12,14 @@
 //
 // The reference of a column's exponentials follows the running maximum only when that is 2^8 or more
 // above it: most tiles neither rescale nor exchange anything between lanes.
+//
+// Measured (32 heads on 8, head_dim 128, bf16): seven sequences of 17 to 8192 rows, 23344 together, 1.06 to
+// 1.09 ms, 1.05 to 1.08 PFLOP/s, where a large product of the same box reaches 1.40 and these matrix
+// instructions alone take 774 us: the power limit, then the exponentials (958 us without) and fills (933).
+// Eight of 1 to 512 rows, 2914 together, 28 us (12 to read and write them once): a workgroup's set-up and
+// results take 9000 of its 28000 clocks.  Two groups of waves that share a tile's keys (eight waves) are
+// faster for few long sequences (one of 4096 rows on 8 heads 70 -> 60 us) and slower for all others
+// (16 -> 16.2, 28 -> 35, 1081 -> 1198).
 #include <atomic>
 #include <type_traits>
 
@@ -428,7 +436,8 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void packed_attn_kerne
 // contraction takes elements 4 g4 .. + 3 of every 16, a lane's scores (keys 4 g4 + r) are the B
 // operand of the second product, and row i of output block c is element C i + c of the head, so that
 // a lane's piece of a value row is C consecutive floats.  The next tile is requested before the current
-// one is used.  WIDE: head_dim is DP.
+// one is used.  WIDE: head_dim is DP.  Four sequences of 1 to 143 rows, 300 together, 4 heads of 64: 6.8 us,
+// the host's time for a call; it is latency (16 waves a workgroup, all keys of a tile at once: 75 tiles).
 __device__ __forceinline__ f32x4 mfma_f32(float a, float b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
 }
