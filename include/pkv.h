@@ -447,7 +447,8 @@ pkv_status pkv_qcache_restore(const pkv_layer_cfg* cfg, const pkv_qcache* cache,
  *     out[i, h] = sum_{t <= row_pos[i]} softmax_t(q[i,h] . K[seq_start[s] + t, g(h)] * scale)
  *                 * V[seq_start[s] + t, g(h)].
  * row_pos[i] < 0: the row attends nothing (an unused slot): out 0, lse -inf.  Rows outside the
- * cache are never read: a sequence ends where the cache does.  Sequences may share rows.
+ * cache are never read: a sequence ends where the cache does, and a seq_start outside of 0 .. rows
+ * counts as the nearer of these.  Sequences may share rows.
  * q, out and lse_out as in pkv_sparse_row_attn (out may be q itself); 16-byte aligned.  fp32
  * softmax and accumulation, one rounding to cfg->dtype.  Meant for few rows a sequence (up to
  * some 64 (row, head of a group) pairs the cache is what is read; beyond, restore it once and use
