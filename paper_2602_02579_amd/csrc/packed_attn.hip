@@ -17,9 +17,8 @@
 // 1.09 ms, 1.05 to 1.08 PFLOP/s, where a large product of the same box reaches 1.40 and these matrix
 // instructions alone take 774 us: the power limit, then the exponentials (958 us without) and fills (933).
 // Eight of 1 to 512 rows, 2914 together, 28 us (12 to read and write them once): a workgroup's set-up and
-// results take 9000 of its 28000 clocks.  Two groups of waves that share a tile's keys (eight waves) are
-// faster for few long sequences (one of 4096 rows on 8 heads 70 -> 60 us) and slower for all others
-// (16 -> 16.2, 28 -> 35, 1081 -> 1198).
+// results take 9000 of its 28000 clocks.  Few and short ones are a chain of half tiles, 1190 clocks each of
+// which the products are 512; nine of 1 to 512 rows, 1800 together, of 8 heads on 2 take 12.8 us.
 #include <atomic>
 #include <type_traits>
 
@@ -54,8 +53,7 @@ struct PackedParams {
 };
 
 constexpr float kLn2 = 0.69314718055994531f;
-constexpr int kCols = 128;     // columns of a workgroup, bf16
-constexpr int kThreads = 256;
+constexpr int kThreads = 256;  // bf16
 
 // What a row sees: keys lo <= t < hi (nothing: hi == 0, and a lo that stays large minus a few tiles)
 __device__ __forceinline__ void keys_of(const int32_t* row_pos, int row, bool valid, int* lo,
@@ -110,21 +108,26 @@ __device__ void attend_alone(const PackedParams<T>& p, int row, int h, int g, in
 }
 
 // DP: head_dim rounded up to 64, 128 or 256.  Elements between are 0 in the queries; in the tiles they
-// repeat others of the same row.
-template <int DP>
-__global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void packed_attn_kernel(PackedParams<bf16_t> p) {
+// repeat others of the same row.  S: 1, or 2 where the tiles are so few that half of the CUs would idle: two
+// waves own 64 columns and every other tile of keys, the other two the rest, and their parts meet in LDS.
+template <int DP, int S>
+__global__ __launch_bounds__(kThreads, DP == 256 || S == 2 ? 1 : 2) void packed_attn_kernel(
+    PackedParams<bf16_t> p) {
+    constexpr int W = 4 / S;                  // waves that go over the same keys
+    constexpr int kCols = 32 * W;
     constexpr int KC = DP / 16;               // contraction steps of a score
     constexpr int DB = DP / 32;               // 32-row blocks of O^T
     constexpr int CH = DP / 8;                // 16-byte pieces of a row
     constexpr int kRow = DP * 2;              // bytes of a row in LDS
     constexpr int kTile = kBN * kRow;         // 64 keys of K or of V
-    constexpr int FILLS = kTile / 1024 / 4;   // instructions of a wave for a tile
+    constexpr int FILLS = kTile / 1024 / W;   // instructions of a wave for a tile
     constexpr int RPI = 64 / CH;              // rows of a fill instruction
-    extern __shared__ __align__(16) unsigned char smem[];
+    extern __shared__ __align__(16) unsigned char smem_all[];
     __shared__ int s_lo[4], s_hi[4];
 
     const int tid = threadIdx.x, lane = tid & 63;
-    const int wave = uniform(tid >> 6);
+    const int wave = uniform(tid >> 6) % W, grp = uniform(tid >> 6) / W;   // of the group; the group
+    unsigned char* const smem = smem_all + grp * 4 * kTile;
     const int hh = lane >> 5, l32 = lane & 31;
     const int g = blockIdx.x % p.hkv;
     const int tile = p.n_tiles - 1 - (int)(blockIdx.x / p.hkv);   // later rows see more: first
@@ -132,10 +135,13 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void packed_attn_kerne
 
     // ---- global -> LDS -----------------------------------------------------------------------------
     // Keys are counted down from the tile's last row: that end is known before anything is read.  Half
-    // tile u holds keys k_end - 32 (u + 1) .. + 31; tile t of values halves 2 t + 1 and 2 t.
+    // tile u of the group holds the 32 keys from key_of(u) on; tile t of values halves 2 t + 1 and 2 t.
     // Piece c of K row r lies at c ^ swizzle: the rows of one operand read are in different banks.  V
     // likewise, for the four rows of a transposing read.
     const int k_end = (int)((min(col0 + kCols, n_cols) - 1) / p.group) + 1;
+    auto key_of = [&](int u) __attribute__((always_inline)) {
+        return k_end - 32 * ((S == 1 ? u : 2 * S * (u >> 1) + 2 * grp + (u & 1)) + 1);
+    };
     auto k_swz = [](int r) { return DP == 64 ? (r >> 1) & 7 : r & 15; };
     auto v_swz = [](int r) { return DP == 64 ? 2 * (r & 2) : 4 * (r & 3); };
     const uint32_t lds = uniform((uint32_t)(uintptr_t)smem);
@@ -144,7 +150,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void packed_attn_kerne
     const uint32_t k_piece = (uint32_t)((lane % CH) ^ k_swz(fill_row)) * 16;
     const uint32_t v_piece = (uint32_t)((lane % CH) ^ v_swz(fill_row)) * 16;
     // instruction i takes rows RPI i further, whose swizzle differs by these bits
-    auto k_bits = [](int i) { return (uint32_t)(DP == 64 ? 64 * (i & 1) : 16 * RPI * i); };
+    auto k_bits = [](int i) { return (uint32_t)(DP == 64 ? 64 * (i & 1) : 16 * (RPI * i & 15)); };
     auto v_bits = [](int i) { return (uint32_t)(DP == 256 ? 128 * (i & 1) : 0); };
     const unsigned char* const k_head = reinterpret_cast<const unsigned char*>(p.k + (int64_t)g * p.D);
     const unsigned char* const v_head = reinterpret_cast<const unsigned char*>(p.v + (int64_t)g * p.D);
@@ -168,17 +174,18 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void packed_attn_kerne
                                 min(piece ^ bits(i), (uint32_t)p.D * 2 - 16), dst + i * 1024);
         }
     };
-    // key halves u and u + 1, of which the upper two waves fill the first; values of tile t
+    // key halves u and u + 1, of which the upper half of the waves fill the first; values of tile t
+    const bool upper = wave >= W / 2;
+    const uint32_t in_half = wave % (W / 2) * FILLS * 1024;
     auto fill_k = [&](int u) {
-        const uint32_t dst =
-            lds + ((u + 1 - (wave >> 1)) & 3) * (kTile / 2) + (wave & 1) * FILLS * 1024;
-        fill(k_head, k_piece, k_bits, dst, k_end - 32 * (u + 2));
+        const uint32_t dst = lds + ((u + (upper ? 0 : 1)) & 3) * (kTile / 2) + in_half;
+        fill(k_head, k_piece, k_bits, dst, upper ? key_of(u) - 32 : key_of(u + 1));
     };
     auto fill_v = [&](int t) {
         fill(v_head, v_piece, v_bits, lds + (2 + (t & 1)) * kTile + wave * FILLS * 1024,
-             k_end - kBN * (t + 1));
+             key_of(2 * t + 1));
     };
-    if (wave >= 2) fill(k_head, k_piece, k_bits, lds + (wave & 1) * FILLS * 1024, k_end - kBN);   // half 0
+    if (upper) fill(k_head, k_piece, k_bits, lds + in_half, key_of(0) - 32);   // half 0
     fill_k(1);
     fill_v(0);
 
@@ -199,8 +206,8 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void packed_attn_kerne
     const int w_lo = min32(lo), w_hi = max32(hi);
     const int in_lo = max32(hi ? lo : 0), in_hi = min32(hi ? hi : 0x7fffffff);
     if (lane == 0) {
-        s_lo[wave] = w_lo;
-        s_hi[wave] = w_hi;
+        s_lo[grp * W + wave] = w_lo;
+        s_hi[grp * W + wave] = w_hi;
     }
 
     // ---- LDS -> operands -----------------------------------------------------------------------------
@@ -227,8 +234,15 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void packed_attn_kerne
     // The scores of the next half tile are multiplied while the exponentials of this one are worked out, its
     // values while the maximum of those scores is found: each matrix instruction has vector instructions
     // to run beside it.  So keys are half a tile ahead of values.
-    const int first = w_hi > w_lo ? (k_end - w_hi) / 32 : 0x7fffffff;    // halves first .. last - 1 hold
-    const int last = w_hi > w_lo ? (k_end - 1 - w_lo) / 32 + 1 : 0;      // keys that some column sees
+    // Halves first .. last - 1 of the group hold keys that some column sees.
+    int first = 0x7fffffff, last = 0;
+    if (w_hi > w_lo) {
+        auto of_group = [&](int n) {          // how many of the workgroup's first n halves
+            return S == 1 ? n : n / (2 * S) * 2 + min(max(n % (2 * S) - 2 * grp, 0), 2);
+        };
+        const int a = of_group((k_end - w_hi) / 32), b = of_group((k_end - 1 - w_lo) / 32 + 1);
+        if (S == 1 || a < b) first = a, last = b;
+    }
     auto k_op = [&](int u, int kc) __attribute__((always_inline)) {
         return *reinterpret_cast<const bf16x8*>(smem + (u & 3) * (kTile / 2) + (kaddr ^ 32 * kc));
     };
@@ -246,7 +260,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void packed_attn_kerne
     };
     // the ends of the columns' keys, and the reference; s: of half u, top: its largest
     auto settle = [&](int u, f32x16& s, float top, auto begins) __attribute__((always_inline)) {
-        const int key0 = k_end - 32 * (u + 1);
+        const int key0 = key_of(u);
         if (__builtin_expect(key0 < in_lo || key0 + 32 > in_hi, 0)) {
             // element r is key 16 (r / 8) + 8 hh + r % 8
             const uint32_t seen = bits_between(lo - key0 - 8 * hh, hi - key0 - 8 * hh);
@@ -348,7 +362,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void packed_attn_kerne
     __syncthreads();
     const int k_lo = uniform(min(min(s_lo[0], s_lo[1]), min(s_lo[2], s_lo[3])));
     const int k_hi = uniform(max(max(s_hi[0], s_hi[1]), max(s_hi[2], s_hi[3])));
-    const int n_iter = k_hi > k_lo ? (k_end - k_lo + kBN - 1) / kBN : 0;
+    const int n_iter = k_hi > k_lo ? (k_end - k_lo + S * kBN - 1) / (S * kBN) : 0;   // both groups
     // tile t begins: its values and the key halves 2 t + 1 and 2 t + 2 are there, everybody is done with
     // what the next fills replace
     auto begin_tile = [&](int t) __attribute__((always_inline)) {
@@ -378,6 +392,33 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void packed_attn_kerne
         }
     }
 
+    // ---- the groups' parts: the second leaves its own in the place of its tiles -------------------------
+    if constexpr (S == 2) {
+        __shared__ float s_m[W][64], s_l[W][64];
+        float* const part = reinterpret_cast<float*>(smem_all + 4 * kTile) + wave * DB * 16 * 64 + lane;
+        wait_vm<0>();
+        __syncthreads();
+        if (grp == 1) {
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) part[(db * 16 + r) * 64] = o_acc[db][r];
+            s_m[wave][lane] = m2;
+            s_l[wave][lane] = l_run;
+        }
+        __syncthreads();
+        if (grp == 1) return;
+        const float mo = s_m[wave][lane], mx = fmaxf(m2, mo), ref = mx == -INFINITY ? 0.f : mx;
+        const float a = __builtin_amdgcn_exp2f(m2 - ref), b = __builtin_amdgcn_exp2f(mo - ref);
+        m2 = mx;
+        l_run = l_run * a + s_l[wave][lane] * b;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                o_acc[db][r] = o_acc[db][r] * a + part[(db * 16 + r) * 64] * b;
+    }
+
     // ---- results: through LDS, so that a column goes out in one piece ------------------------------------
     const float l = l_run + __shfl_xor(l_run, 32);
     const float inv = hi ? 1.f / l : 0.f;
@@ -398,8 +439,10 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void packed_attn_kerne
     const uint32_t alone = (uint32_t)(not_fine | not_fine >> 32);   // by column
     const bool mine = col < n_cols && !(alone >> at & 1);
     const int oc = mine ? row * p.hq + head : -1;
-    wait_vm<0>();                              // (tiles without keys: of the first fills)
-    __syncthreads();
+    if constexpr (S == 1) {
+        wait_vm<0>();                          // (tiles without keys: of the first fills)
+        __syncthreads();
+    }
     unsigned char* const so = smem + wave * 32 * kRow;
 #pragma unroll
     for (int db = 0; db < DB; ++db)
@@ -626,7 +669,6 @@ PackedParams<T> params(const pkv_layer_cfg& cfg, const void* q, const void* k, c
     p.hkv = cfg.n_kv_heads;
     p.group = p.hq / p.hkv;
     p.D = cfg.head_dim;
-    p.n_tiles = (int)ceil_div(m * p.group, kCols);
     p.c2 = scale * 1.4426950408889634f;
     return p;
 }
@@ -642,14 +684,15 @@ bool allow_lds(Kernel kernel, int bytes, std::atomic<bool>* done) {
     return true;
 }
 
-template <int DP>
-pkv_status launch_tiles(const PackedParams<bf16_t>& p, hipStream_t st) {
-    constexpr int kBytes = 4 * kBN * DP * 2;
+template <int DP, int S>
+pkv_status launch_tiles(PackedParams<bf16_t> p, hipStream_t st) {
+    constexpr int kBytes = S * 4 * kBN * DP * 2;
     static std::atomic<bool> done{false};
-    if (!allow_lds(packed_attn_kernel<DP>, kBytes, &done)) return PKV_ERR_LAUNCH;
+    if (!allow_lds(packed_attn_kernel<DP, S>, kBytes, &done)) return PKV_ERR_LAUNCH;
+    p.n_tiles = (int)ceil_div((int64_t)p.m * p.group, 128 / S);
     const int64_t grid = (int64_t)p.n_tiles * p.hkv;
     if (grid >= (int64_t)1 << 24) return PKV_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL(packed_attn_kernel<DP>, dim3((unsigned)grid), dim3(kThreads), kBytes, st, p);
+    hipLaunchKernelGGL((packed_attn_kernel<DP, S>), dim3((unsigned)grid), dim3(kThreads), kBytes, st, p);
     return launch_status();
 }
 
@@ -675,8 +718,15 @@ pkv_status launch_packed_attn(const pkv_layer_cfg& cfg, const void* q, const voi
     const int d = cfg.head_dim;
     if (cfg.dtype == PKV_BF16) {
         const auto p = params<bf16_t>(cfg, q, k, v, row_pos, out, lse_out, m, scale);
-        return d <= 64 ? launch_tiles<64>(p, st)
-                       : d <= 128 ? launch_tiles<128>(p, st) : launch_tiles<256>(p, st);
+        if (d > 128) return launch_tiles<256, 1>(p, st);
+        // Half as wide tiles, their keys split, where all of them run at once (head_dim 128: 128 KB of LDS, one
+        // on a CU).  Then 512 rows of 32 heads on 8 take 10.9 us in place of 13.2, one sequence of 2000 of 8
+        // on 2 25.8 in place of 36.1, four of 512 11.5 and 13.6; where they do not, two of 512 of 32 on 8 take
+        // 17.6 in place of 14.3, eight of 8 on 2 21.9 and 15.4 (one of 4096 alone would gain: 53 and 70).
+        // head_dim 64: 2000 rows of 16 heads on 4 19.5 and 27.9, four of 512 10.7 and 10.6.
+        if (ceil_div(m * p.group, 64) * p.hkv <= (d <= 64 ? 512 : 256))
+            return d <= 64 ? launch_tiles<64, 2>(p, st) : launch_tiles<128, 2>(p, st);
+        return d <= 64 ? launch_tiles<64, 1>(p, st) : launch_tiles<128, 1>(p, st);
     }
     const auto p = params<float>(cfg, q, k, v, row_pos, out, lse_out, m, scale);
     // as many waves as their registers and parts leave room for
