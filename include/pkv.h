@@ -370,7 +370,7 @@ size_t pkv_chunk_attn_workspace_bytes(const pkv_layer_cfg* cfg, int64_t m, int64
  * are as good.  fp32 softmax and accumulation, one rounding to cfg->dtype.  lse_out, if not NULL,
  * receives the natural-log normaliser per (row, head).  out may be q itself and overlaps no
  * other operand.  softmax_scale == 0 means 1/sqrt(D).  All tensors 16-byte aligned
- * (PKV_ERR_UNSUPPORTED otherwise, where m * Hq > 2^31 - 1, and in fp32 where m * Hq / Hkv >= 2^26).
+ * (PKV_ERR_UNSUPPORTED otherwise, where m * Hq > 2^31 - 1, and in fp32 where m * Hq >= 2^27).
  * Scratch: pkv_packed_attn_workspace_bytes.  m == 0 is a no-op.
  */
 pkv_status pkv_packed_attn(const pkv_layer_cfg* cfg,

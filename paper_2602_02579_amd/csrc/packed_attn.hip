@@ -55,6 +55,18 @@ struct PackedParams {
 constexpr float kLn2 = 0.69314718055994531f;
 constexpr int kThreads = 256;  // bf16
 
+// The tile and kv head of a workgroup.  Later rows see more: first.  Where all workgroups run at once, `many`
+// on a CU, every other 256 of them in the opposite order: a CU's are then of different lengths.  (One
+// sequence of 2000 rows in fp32, 4 heads of 64: 41 -> 26 us with the work in front of the loop that went
+// the same step, four of 512 in bf16, 32 heads on 8: 21.5 -> 19.0.)
+__device__ __forceinline__ void job_of(int n_tiles, int hkv, int many, int* tile, int* g) {
+    const int n = gridDim.x, first = blockIdx.x & ~255;
+    int i = blockIdx.x;
+    if (n <= 256 * many && first & 256) i = 2 * first + min(256, n - first) - 1 - i;
+    *g = i % hkv;
+    *tile = n_tiles - 1 - i / hkv;
+}
+
 // What a row sees: keys lo <= t < hi (nothing: hi == 0, and a lo that stays large minus a few tiles)
 __device__ __forceinline__ void keys_of(const int32_t* row_pos, int row, bool valid, int* lo,
                                         int* hi) {
@@ -129,8 +141,8 @@ __global__ __launch_bounds__(kThreads, DP == 256 || S == 2 ? 1 : 2) void packed_
     const int wave = uniform(tid >> 6) % W, grp = uniform(tid >> 6) / W;   // of the group; the group
     unsigned char* const smem = smem_all + grp * 4 * kTile;
     const int hh = lane >> 5, l32 = lane & 31;
-    const int g = blockIdx.x % p.hkv;
-    const int tile = p.n_tiles - 1 - (int)(blockIdx.x / p.hkv);   // later rows see more: first
+    int tile, g;
+    job_of(p.n_tiles, p.hkv, S == 2 || DP == 256 ? 1 : DP == 128 ? 2 : 3, &tile, &g);
     const uint32_t col0 = (uint32_t)tile * kCols, n_cols = (uint32_t)p.m * p.group;
 
     // ---- global -> LDS -----------------------------------------------------------------------------
@@ -474,39 +486,95 @@ __global__ __launch_bounds__(kThreads, DP == 256 || S == 2 ? 1 : 2) void packed_
 }
 
 // ---- fp32 ----------------------------------------------------------------------------------------
-// v_mfma_f32_16x16x4_f32: a workgroup owns 16 columns of a kv head, its NW waves take every NW-th tile of
-// 16 keys and meet in LDS.  Operands come from global memory as they lie there: lane group g4 of a
-// contraction takes elements 4 g4 .. + 3 of every 16, a lane's scores (keys 4 g4 + r) are the B
-// operand of the second product, and row i of output block c is element C i + c of the head, so that
-// a lane's piece of a value row is C consecutive floats.  The next tile is requested before the current
-// one is used.  WIDE: head_dim is DP.  Four sequences of 1 to 143 rows, 300 together, 4 heads of 64: 6.8 us,
-// the host's time for a call; it is latency (16 waves a workgroup, all keys of a tile at once: 75 tiles).
+// v_mfma_f32_16x16x4_f32: a workgroup owns 16 columns of a kv head, its four waves take every fourth tile of
+// 16 keys and meet in LDS; two (head_dim 128) to four (64) workgroups on a CU work while others begin or
+// end.  Operands come from global memory as they lie there: lane group g4 of a contraction takes elements
+// 4 g4 .. + 3 of every 16, a lane's scores (keys 4 g4 + r) are the B operand of the second product, and
+// row i of output block c is element C i + c of the head, so that a lane's piece of a value row is C
+// consecutive floats.  A tile is requested before the one in front of it is used.  WIDE: head_dim is DP.
+//
+// Four sequences of 1 to 143 rows, 300 together, 4 heads of 64: 5.8 us, below the host's time for a call.
+// Sixteen of 512, 8.6 GFLOP: 40 us, 54 TFLOP/s (153 in a large product); one of 2000 25, of 8192 302, 114.
+// Short ones are bound by the 4 us until the first bytes are there; long ones by the matrix pipe.  With
+// 16 waves and one workgroup on a CU four of 512 took 21.8 us in place of 10.6, one of 4096 103 and 80.
+constexpr int kF32Waves = 4;
 __device__ __forceinline__ f32x4 mfma_f32(float a, float b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
 }
 
-template <int DP, int NW, bool WIDE>
-__global__ __launch_bounds__(NW * 64) void packed_attn_f32_kernel(PackedParams<float> p) {
-    constexpr int CM = DP / 16, kColRow = 17;       // 17: the join reads down the columns
+template <int DP, bool WIDE>
+__global__ __launch_bounds__(kF32Waves * 64) void packed_attn_f32_kernel(PackedParams<float> p) {
+    constexpr int NW = kF32Waves, CM = DP / 16, kColRow = 17;       // 17: the join reads down the columns
     extern __shared__ __align__(16) float s_part[];   // [NW][DP][17]
     __shared__ float s_m[NW][16], s_l[NW][16];
     __shared__ int s_col[16][4];                    // row, head, lo, hi
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int g4 = lane >> 4, l16 = lane & 15;
-    const int g = blockIdx.y, D = WIDE ? DP : p.D, C = D / 16;
-    const uint32_t col = (gridDim.x - 1 - blockIdx.x) * 16 + l16;   // later rows first
+    int tile, g;
+    job_of(p.n_tiles, p.hkv, !WIDE || DP == 256 ? 1 : DP == 128 ? 2 : 4, &tile, &g);
+    const int D = WIDE ? DP : p.D, C = D / 16;
+    const uint32_t col = (uint32_t)tile * 16 + l16;
     const int row = col / (uint32_t)p.group, head = g * p.group + (int)(col - (uint32_t)row * p.group);
     const bool valid = row < p.m;
+    // Keys in tiles of 16 counted down from those that hold the last row's: known before anything is read
+    const int last_row = (int)((min((uint32_t)tile * 16 + 16, (uint32_t)p.m * p.group) - 1) / p.group);
+    const int k_end = (last_row | 15) + 1;
+
+    // A tile's keys and values by offsets from its first row, the same ones for every tile; behind the last
+    // row the loads return 0, and in front of the first tile too: no load depends on a condition, so that
+    // none is waited for before its own turn.
+    const int row_bytes = p.hkv * D * 4;
+    const int k_off = l16 * row_bytes + 16 * g4;
+    int v_off[4];   // (an offset for all lanes would not be looked at by the check of the bounds)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v_off[j] = (4 * g4 + j) * row_bytes + 4 * C * l16;
+    const unsigned char* const kb = reinterpret_cast<const unsigned char*>(p.k + (int64_t)g * D);
+    const unsigned char* const vb = reinterpret_cast<const unsigned char*>(p.v + (int64_t)g * D);
+    struct Keys {
+        f32x4 k[CM];
+        float v[4][CM];
+    };
+    auto load = [&](int t0, Keys& x) __attribute__((always_inline)) {
+        const int rows = t0 < 0 ? 0 : min(p.m - t0, 16);
+        const int bytes = rows ? (rows - 1) * row_bytes + 4 * D : 0;
+        const int64_t at = (int64_t)(rows ? t0 : 0) * row_bytes;
+        const auto k = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(kb + at), 0, bytes,
+                                                         0x00027000);
+        const auto v = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(vb + at), 0, bytes,
+                                                         0x00027000);
+#pragma unroll
+        for (int c = 0; c < CM; ++c)
+            if (WIDE || c < C)
+                x.k[c] = __builtin_bit_cast(
+                    f32x4, __builtin_amdgcn_raw_buffer_load_b128(k, k_off + 64 * c, 0, 0));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if constexpr (WIDE) {
+#pragma unroll
+                for (int c = 0; c < CM; c += 4) {
+                    const f32x4 y = __builtin_bit_cast(
+                        f32x4, __builtin_amdgcn_raw_buffer_load_b128(v, v_off[j] + 4 * c, 0, 0));
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x.v[j][c + i] = y[i];
+                }
+            } else {
+#pragma unroll
+                for (int c = 0; c < CM; ++c)
+                    if (c < C)
+                        x.v[j][c] = __uint_as_float(
+                            __builtin_amdgcn_raw_buffer_load_b32(v, v_off[j] + 4 * c, 0, 0));
+            }
+        }
+    };
+    constexpr int kStep = NW * 16;
+    Keys a, b;
+    int t = k_end - 16 * (wave + 1);
+    load(t, a);
+
     int lo, hi;
     keys_of(p.row_pos, row, valid, &lo, &hi);
-    const int k_lo = uniform(min16(lo)), k_hi = uniform(max16(hi));
-
-    const int64_t krow = (int64_t)p.hkv * D;
-    const float* const kb = p.k + (int64_t)g * D + 4 * g4;
-    const float* const vb = p.v + (int64_t)g * D + C * l16;
-    f32x4 q4[CM], k4[CM], kn[CM], o_acc[CM];
-    float v4[4][CM], vn[4][CM];
+    f32x4 q4[CM], o_acc[CM];
     {
         const float* const qp = p.q + ((int64_t)(valid ? row : 0) * p.hq + head) * D + 4 * g4;
 #pragma unroll
@@ -516,51 +584,17 @@ __global__ __launch_bounds__(NW * 64) void packed_attn_f32_kernel(PackedParams<f
             if (valid && (WIDE || c < C)) q4[c] = *reinterpret_cast<const f32x4*>(qp + 16 * c);
         }
     }
-    auto load = [&](int t0) {                       // keys behind the last one repeat it
-        const float* const k = kb + min(t0 + l16, k_hi - 1) * krow;
-#pragma unroll
-        for (int c = 0; c < CM; ++c)
-            if (WIDE || c < C) kn[c] = *reinterpret_cast<const f32x4*>(k + 16 * c);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float* const v = vb + min(t0 + 4 * g4 + j, k_hi - 1) * krow;
-            if constexpr (WIDE) {
-#pragma unroll
-                for (int c = 0; c < CM; c += 4) {
-                    const f32x4 x = *reinterpret_cast<const f32x4*>(v + c);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) vn[j][c + i] = x[i];
-                }
-            } else {
-#pragma unroll
-                for (int c = 0; c < CM; ++c)
-                    if (c < C) vn[j][c] = v[c];
-            }
-        }
-    };
+    const int k_lo = uniform(min16(lo));
     float m2 = -INFINITY, sum = 0.f;                // sum: this lane group's keys only
-    int t0 = k_lo + wave * 16;                      // (nothing to see: k_lo is the largest number)
-    bool more = k_hi > 0 && t0 < k_hi;
-    if (more) load(t0);
-    while (more) {
-#pragma unroll
-        for (int c = 0; c < CM; ++c) k4[c] = kn[c];
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int c = 0; c < CM; ++c) v4[j][c] = vn[j][c];
-        const int t = t0;
-        t0 += NW * 16;
-        more = t0 < k_hi;
-        if (more) load(t0);
+    auto use = [&](int t, const Keys& x) __attribute__((always_inline)) {
         f32x4 s = {0.f, 0.f, 0.f, 0.f}, s2 = s;     // two chains: half the latency
 #pragma unroll
         for (int c = 0; c < CM; ++c)
             if (WIDE || c < C)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    if (c & 1) s2 = mfma_f32(k4[c][j], q4[c][j], s2);
-                    else s = mfma_f32(k4[c][j], q4[c][j], s);
+                    if (c & 1) s2 = mfma_f32(x.k[c][j], q4[c][j], s2);
+                    else s = mfma_f32(x.k[c][j], q4[c][j], s);
                 }
         s += s2;
         float top = -INFINITY;
@@ -590,7 +624,14 @@ __global__ __launch_bounds__(NW * 64) void packed_attn_f32_kernel(PackedParams<f
         for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int c = 0; c < CM; ++c)
-                if (WIDE || c < C) o_acc[c] = mfma_f32(v4[j][c], s[j], o_acc[c]);
+                if (WIDE || c < C) o_acc[c] = mfma_f32(x.v[j][c], s[j], o_acc[c]);
+    };
+    while (t + 16 > k_lo) {
+        load(t - kStep, b);
+        use(t, a);
+        load(t - 2 * kStep, a);
+        if (t - kStep + 16 > k_lo) use(t - kStep, b);
+        t -= 2 * kStep;
     }
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
@@ -611,47 +652,49 @@ __global__ __launch_bounds__(NW * 64) void packed_attn_f32_kernel(PackedParams<f
             for (int r = 0; r < 4; ++r)
                 s_part[(wave * DP + C * (4 * g4 + r) + c) * kColRow + l16] = o_acc[c][r];
     __syncthreads();
-    // a column's elements are written by one wave, so that a row of queries that its result replaces is
+    // All columns at once, TPC threads each: of one wave, so that a row of queries that its result replaces is
     // still there where the column has to be attended alone
-    for (int cc = wave; cc < 16; cc += NW) {
-        const int r = s_col[cc][0], h = s_col[cc][1];
-        if (r < 0) continue;
-        float top = -INFINITY, l = 0.f;
+    constexpr int TPC = NW * 64 / 16, EPT = DP / TPC;
+    const int cc = tid / TPC, e0 = tid % TPC;
+    const int r = s_col[cc][0], h = s_col[cc][1];
+    const bool sees = s_col[cc][3] > 0;
+    float top = -INFINITY, l = 0.f, f[NW], x[EPT];
 #pragma unroll
-        for (int w = 0; w < NW; ++w) top = fmaxf(top, s_m[w][cc]);
-        const float ref = top == -INFINITY ? 0.f : top;
-        float f[NW];
+    for (int w = 0; w < NW; ++w) top = fmaxf(top, s_m[w][cc]);
+    const float ref = top == -INFINITY ? 0.f : top;
 #pragma unroll
-        for (int w = 0; w < NW; ++w) {
-            f[w] = __builtin_amdgcn_exp2f(s_m[w][cc] - ref);
-            l += s_l[w][cc] * f[w];
+    for (int w = 0; w < NW; ++w) {
+        f[w] = __builtin_amdgcn_exp2f(s_m[w][cc] - ref);
+        l += s_l[w][cc] * f[w];
+    }
+    const float inv = sees ? 1.f / l : 0.f;
+    bool fine = !sees || l < INFINITY;
+#pragma unroll
+    for (int i = 0; i < EPT; ++i) {
+        const int d = e0 + i * TPC;
+        x[i] = 0.f;
+        if ((WIDE || d < D) && sees) {
+#pragma unroll
+            for (int w = 0; w < NW; ++w) x[i] += s_part[(w * DP + d) * kColRow + cc] * f[w];
+            x[i] *= inv;
+            fine = fine && fabsf(x[i]) < INFINITY;
         }
-        const bool sees = s_col[cc][3] > 0;
-        const float inv = sees ? 1.f / l : 0.f;
-        const int64_t oc = (int64_t)r * p.hq + h;
-        float x[DP / 64];
-        bool fine = !sees || l < INFINITY;
+    }
+    const uint64_t not_fine = __ballot(!fine && r >= 0);
+    const int64_t oc = (int64_t)r * p.hq + h;
+    if (r >= 0 && !(not_fine >> (lane & ~(TPC - 1)) & ((TPC == 64 ? 0 : 1ull << (TPC & 63)) - 1))) {
 #pragma unroll
-        for (int i = 0; i < DP / 64; ++i) {
-            const int d = lane + 64 * i;
-            x[i] = 0.f;
-            if (d < D && sees) {
-#pragma unroll
-                for (int w = 0; w < NW; ++w) x[i] += s_part[(w * DP + d) * kColRow + cc] * f[w];
-                x[i] *= inv;
-                fine = fine && fabsf(x[i]) < INFINITY;
-            }
-        }
-        if (__any(!fine)) {
-            attend_alone<float, DP>(p, r, h, g, s_col[cc][2], s_col[cc][3]);
-            continue;
-        }
-#pragma unroll
-        for (int i = 0; i < DP / 64; ++i)
-            if (lane + 64 * i < D) p.out[oc * D + lane + 64 * i] = x[i];
-        if (lane == 0 && p.lse)
+        for (int i = 0; i < EPT; ++i)
+            if (WIDE || e0 + i * TPC < D) p.out[oc * D + e0 + i * TPC] = x[i];
+        if (e0 == 0 && p.lse)
             p.lse[oc] = sees ? (top + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
     }
+    if (not_fine)
+        for (int c = 0; c < 64 / TPC; ++c)
+            if (not_fine >> c * TPC & ((TPC == 64 ? 0 : 1ull << (TPC & 63)) - 1)) {
+                const int* const at = s_col[wave * (64 / TPC) + c];
+                attend_alone<float, DP>(p, at[0], at[1], g, at[2], at[3]);
+            }
 }
 
 template <typename T>
@@ -696,15 +739,16 @@ pkv_status launch_tiles(PackedParams<bf16_t> p, hipStream_t st) {
     return launch_status();
 }
 
-template <int DP, int NW, bool WIDE>
-pkv_status launch_f32(const PackedParams<float>& p, hipStream_t st) {
-    constexpr int kBytes = NW * DP * 17 * 4;
+template <int DP, bool WIDE>
+pkv_status launch_f32(PackedParams<float> p, hipStream_t st) {
+    constexpr int kBytes = kF32Waves * DP * 17 * 4;
     static std::atomic<bool> done{false};
-    if (!allow_lds(packed_attn_f32_kernel<DP, NW, WIDE>, kBytes, &done)) return PKV_ERR_LAUNCH;
-    const int64_t tiles = ceil_div((int64_t)p.m * p.group, 16);
-    if (tiles >= 1 << 22 || p.hkv > 65535) return PKV_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL((packed_attn_f32_kernel<DP, NW, WIDE>), dim3((unsigned)tiles, (unsigned)p.hkv),
-                       dim3(NW * 64), kBytes, st, p);
+    if (!allow_lds(packed_attn_f32_kernel<DP, WIDE>, kBytes, &done)) return PKV_ERR_LAUNCH;
+    p.n_tiles = (int)ceil_div((int64_t)p.m * p.group, 16);
+    const int64_t grid = (int64_t)p.n_tiles * p.hkv;
+    if (grid >= 1 << 23) return PKV_ERR_UNSUPPORTED;   // a launch holds less than 2^32 threads
+    hipLaunchKernelGGL((packed_attn_f32_kernel<DP, WIDE>), dim3((unsigned)grid), dim3(kF32Waves * 64), kBytes, st,
+                       p);
     return launch_status();
 }
 
@@ -729,12 +773,11 @@ pkv_status launch_packed_attn(const pkv_layer_cfg& cfg, const void* q, const voi
         return d <= 64 ? launch_tiles<64, 1>(p, st) : launch_tiles<128, 1>(p, st);
     }
     const auto p = params<float>(cfg, q, k, v, row_pos, out, lse_out, m, scale);
-    // as many waves as their registers and parts leave room for
-    if (d == 64) return launch_f32<64, 16, true>(p, st);
-    if (d == 128) return launch_f32<128, 8, true>(p, st);
-    if (d == 256) return launch_f32<256, 4, true>(p, st);
-    if (d < 64) return launch_f32<64, 8, false>(p, st);
-    return d < 128 ? launch_f32<128, 4, false>(p, st) : launch_f32<256, 4, false>(p, st);
+    if (d == 64) return launch_f32<64, true>(p, st);
+    if (d == 128) return launch_f32<128, true>(p, st);
+    if (d == 256) return launch_f32<256, true>(p, st);
+    if (d < 64) return launch_f32<64, false>(p, st);
+    return d < 128 ? launch_f32<128, false>(p, st) : launch_f32<256, false>(p, st);
 }
 
 }  // namespace pkv

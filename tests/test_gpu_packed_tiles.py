@@ -11,7 +11,8 @@ pytestmark = pytest.mark.gpu
 
 # 12000 or 70000 (row, head) pairs: less and more than 256 (head_dim 64: 512) tiles of 64
 LAYOUTS = [("bf16", 32, 8, 128), ("bf16", 24, 8, 48), ("bf16", 16, 4, 96), ("bf16", 40, 8, 64),
-           ("bf16", 8, 8, 112), ("bf16", 7, 1, 128)]
+           ("bf16", 8, 8, 112), ("bf16", 7, 1, 128),
+           ("f32", 8, 8, 64), ("f32", 16, 4, 128), ("f32", 10, 2, 48), ("f32", 12, 4, 112), ("f32", 8, 2, 256)]
 
 
 def lengths(hq, many):
