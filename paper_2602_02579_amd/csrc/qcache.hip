@@ -41,7 +41,8 @@ __device__ __forceinline__ void decode8(uint32_t c, float scale, float* x) {
 // rows that follow each other in the cache are then written in runs of hundreds of bytes, codes and
 // scales (a workgroup for all heads of few tokens wrote value scales byte by byte into 64 lines:
 // 32k tokens of 8 heads of 128 43 us).  blockIdx.z: keys or values.  Bound by the bytes: 32k tokens of 8
-// heads of 128 in bf16, 134 MB in and 38 MB out, 32.4 us, 5.3 TB/s (a large copy: 5.1).
+// heads of 128 in bf16, 134 MB in and 38 MB out, 32.4 us, 5.3 TB/s (a large copy: 5.1; with two, four and
+// eight tokens a thread 32.4, 33.2 and 34.3).
 template <typename T>
 __global__ __launch_bounds__(256) void qcache_store_kernel(const T* __restrict__ k,
                                                            const T* __restrict__ v,
@@ -84,8 +85,9 @@ __global__ __launch_bounds__(256) void qcache_store_kernel(const T* __restrict__
 
 // A thread owns, for one token, 8 pairs of elements (i, i + D / 2) and walks over heads_each heads:
 // sines and cosines are worked out once, under the latency of the first heads' bytes.  blockIdx.y: which
-// heads, blockIdx.z: keys or values.  Bound by the bytes: 32k tokens of 8 heads of 128 to bf16, 38 MB in and
-// 134 MB out, 28.0 us, 6.1 TB/s; 7 chunks of 512 out of a store 6.8 us, of which the bytes are 3.7.
+// heads, blockIdx.z: keys or values.  Bound by the bytes written: 32k tokens of 8 heads of 128 to bf16, 38 MB in
+// and 134 MB out, 28 us out of a warm cache, 38 out of a cold one, however the heads and the stores are laid
+// out; 7 chunks of 512 out of a store 6.9 us, of which the bytes are 3.7.
 template <typename T>
 __global__ __launch_bounds__(256) void qcache_restore_kernel(
     pkv_qcache cache, const int32_t* __restrict__ row_idx, const int32_t* __restrict__ pos,

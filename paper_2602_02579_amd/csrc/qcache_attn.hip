@@ -16,7 +16,7 @@
 // (24 bits), so the products are as exact as fp32 ones.
 //
 // What bounds it: reading the cache, 4.5 bits an element, from some 64k rows on: one row over 131328 keys
-// of 8 heads of 128, 151 MB, 28.3 us, 5.3 TB/s.  Below, the vector unit and the start: 32896 keys 10.6 us
+// of 8 heads of 128, 151 MB, 28.3 us, 5.3 TB/s.  Below, the vector unit and the start: 32896 keys 10.2 us
 // (7.4 are the bytes).  32 keys are some 139 vector instructions, 650 clocks, of which 64 convert codes
 // and 32 bring two keys of an element together; a SIMD has two waves of them, and the first bytes come
 // after 4 us.  16 sequences of 0 to 12033 rows, 65 MB, 16.4 us (12.8).
