@@ -15,11 +15,12 @@
 // Every value of the format is exact in bf16.  fp32: queries and weights go in as three bf16 parts
 // (24 bits), so the products are as exact as fp32 ones.
 //
-// What bounds it: reading the cache, 4.5 bits an element, from some 64k rows on: one row over 131328 keys
-// of 8 heads of 128, 151 MB, 28.3 us, 5.3 TB/s.  Below, the vector unit and the start: 32896 keys 10.2 us
-// (7.4 are the bytes).  32 keys are some 139 vector instructions, 650 clocks, of which 64 convert codes
-// and 32 bring two keys of an element together; a SIMD has two waves of them, and the first bytes come
-// after 4 us.  16 sequences of 0 to 12033 rows, 65 MB, 16.4 us (12.8).
+// What bounds it: reading the cache, 4.5 bits an element.  One row over 131328 keys of 8 heads of 128, 151 MB,
+// 28.3 us, 5.3 TB/s; over 32896 10.2 us, of which the bytes are 7.4 at a large copy's rate; 16 sequences of 0 to
+// 12033 rows, 65 MB, 16.4 us (12.8).  The requests leave 1.1 us after a workgroup's start (several sequences:
+// 2.2), the first bytes are there after 4, and the waves meet for 0.6.  32 keys are some 139 vector
+// instructions, of which 64 convert codes and 32 bring two keys of an element together; without the
+// latter the batch would take 0.6 us less.
 //
 // The reference of a column's exponentials follows the running maximum only when that is 2^8 or more
 // above it: few steps rescale, and the lanes of a column need not meet every step.
