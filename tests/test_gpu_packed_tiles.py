@@ -4,8 +4,9 @@ keys are split within a workgroup): what the smaller problems check, in both for
 import pytest
 import torch
 
+from paper_2602_02579_amd import api
 from tests import attention64 as A
-from tests.test_gpu_packed_attn import check, problem, run
+from tests.test_gpu_packed_attn import DT, check, problem, run
 
 pytestmark = pytest.mark.gpu
 
@@ -62,3 +63,20 @@ def test_what_a_row_does_not_see_does_not_reach_it(gpu_device, many, bad):
     want = A.attention(q, k, v, at - pos, at + 1)
     A.agree(got[0][clean], got[1][clean], [x[clean] for x in want], "bf16", max(lens), 128)
     assert torch.isnan(got[0][301:342]).all()
+
+
+@pytest.mark.parametrize("dtype,hkv", [("bf16", 16), ("f32", 8)])
+def test_offsets_beyond_32_bits(gpu_device, dtype, hkv):
+    """Tensors of more than 4 GB: a window of 41 rows for every row, looked at where they end."""
+    m = (1 << 20) + 4099
+    cfg = api.LayerCfg(hkv, hkv, 128, 64, 1e4, dtype)
+    gen = torch.Generator(device=gpu_device).manual_seed(1)
+    q, k, v = (torch.empty((m, hkv, 128), dtype=DT[dtype], device=gpu_device).normal_(generator=gen)
+               for _ in range(3))
+    pos = torch.arange(m, dtype=torch.int32, device=gpu_device).clamp(max=40)
+    out, lse = run(cfg, q, k, v, pos)
+    for a in (0, m // 2 + 1, m - 500):
+        rows, seen = slice(a, a + 500), slice(max(0, a - 40), a + 500)
+        at = torch.arange(a, a + 500, device=gpu_device) - seen.start
+        want = A.attention(q[rows], k[seen], v[seen], at - pos[rows], at + 1)
+        A.agree(out[rows], lse[rows], want, dtype, 41, 128)
