@@ -582,20 +582,26 @@ def pkv_query_score_lse(cfg: LayerCfg, q: torch.Tensor, k: torch.Tensor, lse: to
 # ---- packed prompts, the cache in 4 bits -------------------------------------------
 
 # These calls run on the current device and refuse tensors of another one; one look at a tensor's
-# device serves both checks (the binding's time is of the order of a small launch).
+# device serves both checks.  The binding's time is of the order of a small launch, so what holds for
+# tensors that fit is asked where the call is (7.1 -> 6.5 us a call); _refuse says what does not.
 def _device_of_call(t: torch.Tensor) -> int:
     return torch.cuda.current_device() if t.is_cuda else -2
 
 
-# the same number without a look at whether CUDA is initialised: t is on the GPU
-if hasattr(torch._C, "_cuda_getDevice"):
+def _stream_of(device: int) -> int:
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+# the same numbers without a look at whether CUDA is initialised (t is on the GPU) or a Stream object
+if hasattr(torch._C, "_cuda_getCurrentRawStream") and hasattr(torch._C, "_cuda_getDevice"):
     def _device_of_call(t: torch.Tensor) -> int:   # noqa: F811
         return torch._C._cuda_getDevice() if t.is_cuda else -2
 
+    def _stream_of(device: int) -> int:   # noqa: F811
+        return torch._C._cuda_getCurrentRawStream(device)
 
-def _own(t: Optional[torch.Tensor], dtype: torch.dtype, name: str, device: int):
-    if t is None:
-        return None
+
+def _own(t: torch.Tensor, dtype: torch.dtype, name: str, device: int):
     if t.get_device() != device:
         raise ValueError(f"{name} must be a GPU tensor of the current device")
     if t.dtype != dtype:
@@ -605,9 +611,12 @@ def _own(t: Optional[torch.Tensor], dtype: torch.dtype, name: str, device: int):
     return t.data_ptr()
 
 
-def _own_ws(ws: Optional[torch.Tensor], device: int):
-    if ws is None:
-        return None, 0
+def _refuse(device: int, *named) -> None:
+    for t, dtype, name in named:
+        _own(t, dtype, name, device)
+
+
+def _own_ws(ws: torch.Tensor, device: int):
     if ws.get_device() != device or not ws.is_contiguous():
         raise ValueError("workspace must be a contiguous GPU tensor of the current device")
     return ws.data_ptr(), ws.numel() * ws.element_size()
@@ -629,11 +638,18 @@ def pkv_packed_attn(cfg: LayerCfg, q: torch.Tensor, k: torch.Tensor, v: torch.Te
     if lse_out is not None and lse_out.shape != (m, hq):
         raise ValueError("lse_out must be [m, Hq]")
     dev = _device_of_call(q)
-    wp, wb = _own_ws(ws, dev)
+    if not (q.dtype is dt and k.dtype is dt and v.dtype is dt and out.dtype is dt
+            and row_pos.dtype is torch.int32 and q.get_device() == dev and k.get_device() == dev
+            and v.get_device() == dev and out.get_device() == dev and row_pos.get_device() == dev
+            and q.is_contiguous() and k.is_contiguous() and v.is_contiguous()
+            and out.is_contiguous() and row_pos.is_contiguous()):
+        _refuse(dev, (q, dt, "q"), (k, dt, "k"), (v, dt, "v"), (row_pos, torch.int32, "row_pos"),
+                (out, dt, "out"))
+    wp, wb = (None, 0) if ws is None else _own_ws(ws, dev)
     _check("pkv_packed_attn", load_library().pkv_packed_attn(
-        cfg._ref, _own(q, dt, "q", dev), _own(k, dt, "k", dev), _own(v, dt, "v", dev),
-        _own(row_pos, torch.int32, "row_pos", dev), _own(out, dt, "out", dev),
-        _own(lse_out, torch.float32, "lse_out", dev), m, softmax_scale, wp, wb, _stream()))
+        cfg._ref, q.data_ptr(), k.data_ptr(), v.data_ptr(), row_pos.data_ptr(), out.data_ptr(),
+        None if lse_out is None else _own(lse_out, torch.float32, "lse_out", dev), m,
+        softmax_scale, wp, wb, _stream_of(dev)))
 
 
 class QCache:
@@ -689,9 +705,13 @@ def pkv_qcache_store(cfg: LayerCfg, k: torch.Tensor, v: torch.Tensor, cache: QCa
     if dst_row is not None and dst_row.shape != (m,):
         raise ValueError("dst_row must be [m]")
     dev = _device_of_call(k)
+    if not (k.dtype is dt and v.dtype is dt and k.get_device() == dev and v.get_device() == dev
+            and k.is_contiguous() and v.is_contiguous()):
+        _refuse(dev, (k, dt, "k"), (v, dt, "v"))
     _check("pkv_qcache_store", load_library().pkv_qcache_store(
-        cfg._ref, _own(k, dt, "k", dev), _own(v, dt, "v", dev),
-        _own(dst_row, torch.int32, "dst_row", dev), _of_cache(cfg, cache, dev), m, _stream()))
+        cfg._ref, k.data_ptr(), v.data_ptr(),
+        None if dst_row is None else _own(dst_row, torch.int32, "dst_row", dev),
+        _of_cache(cfg, cache, dev), m, _stream_of(dev)))
 
 
 def pkv_qcache_restore(cfg: LayerCfg, cache: QCache, k_out: torch.Tensor, v_out: torch.Tensor,
@@ -706,10 +726,14 @@ def pkv_qcache_restore(cfg: LayerCfg, cache: QCache, k_out: torch.Tensor, v_out:
     if pos is not None and pos.shape != (m,):
         raise ValueError("pos must be [m]")
     dev = _device_of_call(k_out)
+    if not (k_out.dtype is dt and v_out.dtype is dt and k_out.get_device() == dev
+            and v_out.get_device() == dev and k_out.is_contiguous() and v_out.is_contiguous()):
+        _refuse(dev, (k_out, dt, "k_out"), (v_out, dt, "v_out"))
     _check("pkv_qcache_restore", load_library().pkv_qcache_restore(
-        cfg._ref, _of_cache(cfg, cache, dev), _own(row_idx, torch.int32, "row_idx", dev),
-        _own(pos, torch.int32, "pos", dev), int(pos_base), bool(rotate),
-        _own(k_out, dt, "k_out", dev), _own(v_out, dt, "v_out", dev), m, _stream()))
+        cfg._ref, _of_cache(cfg, cache, dev),
+        None if row_idx is None else _own(row_idx, torch.int32, "row_idx", dev),
+        None if pos is None else _own(pos, torch.int32, "pos", dev), int(pos_base), bool(rotate),
+        k_out.data_ptr(), v_out.data_ptr(), m, _stream_of(dev)))
 
 
 def pkv_qcache_attn_workspace_bytes(cfg: LayerCfg, rows: int, m: int, n_seq: int = 1) -> int:
@@ -729,12 +753,16 @@ def pkv_qcache_attn(cfg: LayerCfg, q: torch.Tensor, cache: QCache, row_pos: torc
     if lse_out is not None and lse_out.shape != (m, hq):
         raise ValueError("lse_out must be [m, Hq]")
     dev = _device_of_call(q)
-    wp, wb = _own_ws(ws, dev)
+    if not (q.dtype is dt and out.dtype is dt and row_pos.dtype is torch.int32
+            and q.get_device() == dev and out.get_device() == dev and row_pos.get_device() == dev
+            and q.is_contiguous() and out.is_contiguous() and row_pos.is_contiguous()):
+        _refuse(dev, (q, dt, "q"), (row_pos, torch.int32, "row_pos"), (out, dt, "out"))
+    wp, wb = (None, 0) if ws is None else _own_ws(ws, dev)
     _check("pkv_qcache_attn", load_library().pkv_qcache_attn(
-        cfg._ref, _own(q, dt, "q", dev), _of_cache(cfg, cache, dev),
-        _own(row_pos, torch.int32, "row_pos", dev),
-        _own(seq_start, torch.int32, "seq_start", dev), _own(out, dt, "out", dev),
-        _own(lse_out, torch.float32, "lse_out", dev), m, n_seq, softmax_scale, wp, wb, _stream()))
+        cfg._ref, q.data_ptr(), _of_cache(cfg, cache, dev), row_pos.data_ptr(),
+        None if seq_start is None else _own(seq_start, torch.int32, "seq_start", dev),
+        out.data_ptr(), None if lse_out is None else _own(lse_out, torch.float32, "lse_out", dev),
+        m, n_seq, softmax_scale, wp, wb, _stream_of(dev)))
 
 
 # ---- layer glue -------------------------------------------------------------------

@@ -494,8 +494,9 @@ __global__ __launch_bounds__(kThreads, DP == 256 || S == 2 ? 1 : 2) void packed_
 // consecutive floats.  A tile is requested before the one in front of it is used.  WIDE: head_dim is DP.
 //
 // Four sequences of 1 to 143 rows, 300 together, 4 heads of 64: 5.8 us, below the host's time for a call.
-// Sixteen of 512, 8.6 GFLOP: 40 us, 54 TFLOP/s (153 in a large product); one of 2000 25, of 8192 302, 114.
-// Short ones are bound by the 4 us until the first bytes are there; long ones by the matrix pipe.  With
+// Sixteen of 512, 2.1 GFLOP: 40 us, 54 TFLOP/s (153 in a large product); one of 2000 25, of 8192 302, 114.
+// Few short ones are bound by the 1.5 us until the first bytes are there and the steps behind one another;
+// many by the bytes that every tile reads from L2 (12 TB/s) and, as much, by the products.  With
 // 16 waves and one workgroup on a CU four of 512 took 21.8 us in place of 10.6, one of 4096 103 and 80.
 constexpr int kF32Waves = 4;
 __device__ __forceinline__ f32x4 mfma_f32(float a, float b, f32x4 c) {
