@@ -45,7 +45,6 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kWaves = 8;
 constexpr int kGroup = kWaves * 32;   // keys of a workgroup's step
-constexpr int kJoinWaves = 8;
 constexpr float kLn2 = 0.69314718055994531f;
 
 struct QAttnParams {
@@ -625,9 +624,9 @@ __global__ __launch_bounds__(kWaves * 64) void qcache_attn_kernel(QAttnParams p)
     }
 }
 
-// A row and head of which several workgroups hold parts: eight waves share the parts and meet; rows
-// of sequences without keys, which nobody took, are written here too.
-template <typename T>
+// A row and head of which several workgroups hold parts: the waves share the parts and meet; rows of
+// sequences without keys, which nobody took, are written here too.
+template <typename T, int kJoinWaves>
 __global__ __launch_bounds__(kJoinWaves * 64) void qcache_attn_join_kernel(QAttnParams p) {
     __shared__ float s_o[kJoinWaves][256];
     __shared__ float2 s_ml[kJoinWaves];
@@ -744,6 +743,13 @@ pkv_status launch_main(const QAttnParams& p, int nc, dim3 grid, hipStream_t st) 
     return launch_main<T, 64, 1>(p, grid, st);
 }
 
+template <typename T, int WAVES>
+pkv_status launch_join(const QAttnParams& p, int64_t m, hipStream_t st) {
+    hipLaunchKernelGGL((qcache_attn_join_kernel<T, WAVES>), dim3((unsigned)(m * p.hq)), dim3(WAVES * 64), 0,
+                       st, p);
+    return launch_status();
+}
+
 struct QPlan {
     int nc, log2_wg;
     int64_t tiles;
@@ -811,12 +817,16 @@ pkv_status launch_qcache_attn(const pkv_layer_cfg& cfg, const void* q, const pkv
                                    : launch_main<float>(p, pl.nc, grid, st);
     if (status != PKV_OK) return status;
     if (n_seq == 1 && p.n_wg == 1) return PKV_OK;
-    const dim3 rows_heads((unsigned)(m * cfg.n_q_heads));
-    if (bf16)
-        hipLaunchKernelGGL((qcache_attn_join_kernel<bf16_t>), rows_heads, dim3(kJoinWaves * 64), 0, st, p);
-    else
-        hipLaunchKernelGGL((qcache_attn_join_kernel<float>), rows_heads, dim3(kJoinWaves * 64), 0, st, p);
-    return launch_status();
+    // Waves for the parts that a row has: a dozen or more on average, a few, hardly any where there are more
+    // sequences than workgroups (but a thread for each element).  Eight, four and two waves: one sequence of
+    // 131328 rows 31.2, 31.8 and 33.1 us, 9 of 100 to 5000 on 128 workgroups 11.6, 12.0 and 12.3, 16 of 0 to
+    // 12033 on 32 20.1, 19.8 and 19.6, four with four rows each 18.1, 17.3 and 17.9, 100 of 300 27.6, 25.5
+    // and 24.4.
+    if (n_seq * 12 <= p.n_wg || n_seq == 1)
+        return bf16 ? launch_join<bf16_t, 8>(p, m, st) : launch_join<float, 8>(p, m, st);
+    if (n_seq <= p.n_wg || p.D > 128)
+        return bf16 ? launch_join<bf16_t, 4>(p, m, st) : launch_join<float, 4>(p, m, st);
+    return bf16 ? launch_join<bf16_t, 2>(p, m, st) : launch_join<float, 2>(p, m, st);
 }
 
 }  // namespace pkv
