@@ -367,7 +367,9 @@ size_t pkv_chunk_attn_workspace_bytes(const pkv_layer_cfg* cfg, int64_t m, int64
  *     out[i, h] = sum_{i - row_pos[i] <= t <= i} softmax_t(q[i,h] . k[t,g(h)] * scale) * v[t, g(h)].
  * A row with row_pos[i] < 0 attends nothing (padding): out 0, lse -inf.  Positions beyond i count
  * as i, so any value is safe; positions that do not begin anew (a window of w rows: min(pos, w - 1))
- * are as good.  fp32 softmax and accumulation, one rounding to cfg->dtype.  lse_out, if not NULL,
+ * are as good.  fp32 softmax and accumulation, one rounding to cfg->dtype.  Values that are not finite
+ * reach the same element of the rows that see them, keys that are not their whole rows, and no
+ * others (which costs several times the call without them).  lse_out, if not NULL,
  * receives the natural-log normaliser per (row, head).  out may be q itself and overlaps no
  * other operand.  softmax_scale == 0 means 1/sqrt(D).  All tensors 16-byte aligned
  * (PKV_ERR_UNSUPPORTED otherwise, where m * Hq > 2^31 - 1, and in fp32 where m * Hq >= 2^27).

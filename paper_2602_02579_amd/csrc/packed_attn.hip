@@ -79,44 +79,179 @@ __device__ __forceinline__ void keys_of(const int32_t* row_pos, int row, bool va
     *hi = row + 1;
 }
 
-// One (row, head) by a wave, key by key, nothing but the keys that it sees: for columns whose result is
-// not finite.  A value that is not finite in a key of the tile that the column does not see comes
-// into the products above as 0 times infinity; here it does not.
-template <typename T, int DP>
-__device__ void attend_alone(const PackedParams<T>& p, int row, int h, int g, int lo, int hi) {
-    constexpr int E = DP / 64;
-    const int lane = threadIdx.x & 63;
-    const int64_t o = ((int64_t)row * p.hq + h) * p.D;
-    float q[E], acc[E], mx = -INFINITY, sum = 0.f;
+// Columns whose result is not finite though their weights are.  A value of a tile that is not finite comes into
+// the products as 0 times infinity for the columns that do not see it, and sums of large values may leave
+// the range before they are divided.  So those columns are attended once more by their wave, with
+// weights that are divided first (a sum is then no larger than the values), values that are not finite left
+// out of the products, and what the column sees of these counted by products with 1 for every key that
+// is seen: an element is infinite or NaN where a seen value is.  Keys and values come straight from global
+// memory, 32 (fp32: 16) at a time, and values element by element: one NaN that all of 8192 rows of 32 heads on 8
+// see makes 3.2 ms of 0.53, NaN in all values 5.5 (fp32, 4 heads of 64: 3.1 and 4.8 of 0.33).  Columns whose
+// weights are not finite (a key or query that is not) do not come here: they are NaN.
+// ref, inv: of the column, the reference of its exponentials and 1 / their sum; mine: it is one of these.
+__device__ __forceinline__ float seen_value(float x, bool plus, bool minus) {
+    return plus ? (minus ? __builtin_nanf("") : INFINITY) : minus ? -INFINITY : x;
+}
+
+template <int DP>
+__device__ __forceinline__ void attend_again(const PackedParams<bf16_t>& p, int row, int head, int g,
+                                             int lo, int hi, float ref, float inv, bool mine) {
+    constexpr int KC = DP / 16, DB = DP / 32;
+    const int lane = threadIdx.x & 63, hh = lane >> 5, l32 = lane & 31;
+    if (!mine) lo = 0x7fff0000, hi = 0;
+    const int prow = (l32 & 0x13) | ((l32 & 4) << 1) | ((l32 & 8) >> 1);   // swap_bits_2_3, as below
+    const int64_t row_len = (int64_t)p.hkv * p.D;
+    const uint16_t* const vh = reinterpret_cast<const uint16_t*>(p.v) + (int64_t)g * p.D;
+    bf16_t* const out = p.out + ((int64_t)row * p.hq + head) * p.D;
+    bf16x8 q[KC];
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-        q[e] = lane + 64 * e < p.D ? Elem<T>::load(p.q + o + lane + 64 * e) : 0.f;
-        acc[e] = 0.f;
+    for (int kc = 0; kc < KC; ++kc)      // (out may be q: the other columns' are results by now)
+        q[kc] = mine && kc * 16 < p.D
+                    ? *reinterpret_cast<const bf16x8*>(
+                          p.q + ((int64_t)row * p.hq + head) * p.D + kc * 16 + hh * 8)
+                    : bf16x8{};
+    f32x16 o[DB];
+    uint32_t plus[DB], minus[DB];        // bit r: of o[.][r]
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+        plus[db] = minus[db] = 0;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[db][r] = 0.f;
     }
-    for (int t = lo; t < hi; ++t) {
-        const int64_t at = ((int64_t)t * p.hkv + g) * p.D;
-        float s = 0.f;
+    const int end = max32(hi);
+#pragma unroll 1
+    for (int key0 = min32(lo) & ~31; key0 < end; key0 += 32) {
+        const bf16_t* const kp = p.k + min(key0 + prow, p.m - 1) * row_len + (int64_t)g * p.D + hh * 8;
+        f32x16 s;
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-            if (lane + 64 * e < p.D) s += q[e] * Elem<T>::load(p.k + at + lane + 64 * e);
+        for (int r = 0; r < 16; ++r) s[r] = 0.f;
 #pragma unroll
-        for (int x = 32; x > 0; x >>= 1) s += __shfl_xor(s, x);
-        s *= p.c2;
-        const float m = fmaxf(mx, s), ref = m == -INFINITY ? 0.f : m;
-        const float corr = __builtin_amdgcn_exp2f(mx - ref), w = __builtin_amdgcn_exp2f(s - ref);
-        mx = m;
-        sum = sum * corr + w;
+        for (int kc = 0; kc < KC; ++kc)
+            if (kc * 16 < p.D) s = mfma32(*reinterpret_cast<const bf16x8*>(kp + kc * 16), q[kc], s);
+        const uint32_t bits = bits_between(lo - key0 - 8 * hh, hi - key0 - 8 * hh);
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-            if (lane + 64 * e < p.D) acc[e] = acc[e] * corr + w * Elem<T>::load(p.v + at + lane + 64 * e);
+        for (int kb = 0; kb < 2; ++kb) {             // 16 keys, 8 of them this lane's
+            bf16x8 w, seen;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const bool on = bits >> (16 * kb + e) & 1;
+                w[e] = (bf16_t)(on ? __builtin_amdgcn_exp2f(fmaf(s[8 * kb + e], p.c2, -ref)) * inv : 0.f);
+                seen[e] = (bf16_t)(on ? 1.f : 0.f);
+            }
+#pragma unroll
+            for (int db = 0; db < DB; ++db) {
+                const int d = db * 32 + l32;
+                bf16x8 v, is_plus, is_minus;
+                bool any = false;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int t = min(key0 + 16 * kb + 8 * hh + e, p.m - 1);
+                    const uint16_t x = d < p.D ? vh[t * row_len + d] : 0;
+                    const bool off = (x & 0x7f80) == 0x7f80, nan = off && (x & 0x7f);
+                    v[e] = __builtin_bit_cast(bf16_t, off ? (uint16_t)0 : x);
+                    is_plus[e] = (bf16_t)(nan || x == 0x7f80 ? 1.f : 0.f);
+                    is_minus[e] = (bf16_t)(nan || x == 0xff80 ? 1.f : 0.f);
+                    any = any || off;
+                }
+                o[db] = mfma32(v, w, o[db]);
+                if (__any(any)) {
+                    f32x16 n;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) n[r] = 0.f;
+                    const f32x16 up = mfma32(is_plus, seen, n), down = mfma32(is_minus, seen, n);
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        plus[db] |= (uint32_t)(up[r] > 0.f) << r;
+                        minus[db] |= (uint32_t)(down[r] > 0.f) << r;
+                    }
+                }
+            }
+        }
     }
+    if (!mine) return;
 #pragma unroll
-    for (int e = 0; e < E; ++e)
-        if (lane + 64 * e < p.D)
-            p.out[o + lane + 64 * e] = Elem<T>::from_f32(lo < hi ? acc[e] / sum : 0.f);
-    if (lane == 0 && p.lse)
-        p.lse[(int64_t)row * p.hq + h] =
-            lo < hi ? (mx + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4) {
+            const int d = db * 32 + r4 * 8 + hh * 4;
+            bf16x4 x;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int r = 4 * r4 + e;
+                x[e] = (bf16_t)seen_value(o[db][r], plus[db] >> r & 1, minus[db] >> r & 1);
+            }
+            if (d < p.D) *reinterpret_cast<bf16x4*>(out + d) = x;
+        }
+}
+
+__device__ __forceinline__ f32x4 mfma_f32(float a, float b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
+}
+
+template <int DP>
+__device__ __forceinline__ void attend_again_f32(const PackedParams<float>& p, int row, int head,
+                                                 int g, int lo, int hi, float ref, float inv,
+                                                 bool mine) {
+    constexpr int CM = DP / 16;
+    const int lane = threadIdx.x & 63, g4 = lane >> 4, l16 = lane & 15, C = p.D / 16;
+    if (!mine) lo = 0x7fff0000, hi = 0;
+    const int64_t row_len = (int64_t)p.hkv * p.D;
+    float* const out = p.out + ((int64_t)row * p.hq + head) * p.D;
+    f32x4 q[CM], o[CM];
+    uint32_t plus[CM], minus[CM];
+#pragma unroll
+    for (int c = 0; c < CM; ++c) {
+        o[c] = q[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+        plus[c] = minus[c] = 0;
+        if (mine && c < C)
+            q[c] = *reinterpret_cast<const f32x4*>(p.q + ((int64_t)row * p.hq + head) * p.D + 16 * c +
+                                                   4 * g4);
+    }
+    const int end = uniform(max16(hi));
+#pragma unroll 1
+    for (int t0 = uniform(min16(lo)) & ~15; t0 < end; t0 += 16) {
+        const float* const kp = p.k + min(t0 + l16, p.m - 1) * row_len + (int64_t)g * p.D + 4 * g4;
+        f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < CM; ++c)
+            if (c < C) {
+                const f32x4 k = *reinterpret_cast<const f32x4*>(kp + 16 * c);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s = mfma_f32(k[j], q[c][j], s);
+            }
+        const uint32_t bits = bits_between(lo - t0 - 4 * g4, hi - t0 - 4 * g4);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const bool on = bits >> j & 1;
+            const float w = on ? __builtin_amdgcn_exp2f(s[j] * p.c2 - ref) * inv : 0.f, seen = on ? 1.f : 0.f;
+            const float* const vp = p.v + min(t0 + 4 * g4 + j, p.m - 1) * row_len + (int64_t)g * p.D +
+                                    C * l16;
+#pragma unroll
+            for (int c = 0; c < CM; ++c)
+                if (c < C) {
+                    const float x = vp[c];
+                    const bool off = !(fabsf(x) < INFINITY);
+                    o[c] = mfma_f32(off ? 0.f : x, w, o[c]);
+                    if (__any(off)) {
+                        const f32x4 n = {0.f, 0.f, 0.f, 0.f};
+                        const f32x4 up = mfma_f32(off && !(x < 0.f) ? 1.f : 0.f, seen, n);
+                        const f32x4 down = mfma_f32(off && !(x > 0.f) ? 1.f : 0.f, seen, n);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            plus[c] |= (uint32_t)(up[r] > 0.f) << r;
+                            minus[c] |= (uint32_t)(down[r] > 0.f) << r;
+                        }
+                    }
+                }
+        }
+    }
+    if (!mine) return;
+#pragma unroll
+    for (int c = 0; c < CM; ++c)
+        if (c < C)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                out[C * (4 * g4 + r) + c] = seen_value(o[c][r], plus[c] >> r & 1, minus[c] >> r & 1);
 }
 
 // DP: head_dim rounded up to 64, 128 or 256.  Elements between are 0 in the queries; in the tiles they
@@ -447,9 +582,11 @@ __global__ __launch_bounds__(kThreads, DP == 256 || S == 2 ? 1 : 2) void packed_
     not_ahead(at);
     const uint32_t col = col0 + wave * 32 + at;
     const int row = col / (uint32_t)p.group, head = g * p.group + (int)(col - (uint32_t)row * p.group);
-    const uint64_t not_fine = __ballot(check != 0.f && col < n_cols);
-    const uint32_t alone = (uint32_t)(not_fine | not_fine >> 32);   // by column
-    const bool mine = col < n_cols && !(alone >> at & 1);
+    // not finite: NaN where the weights are, otherwise attended once more
+    const bool again = check != 0.f && col < n_cols && (l > 0.f || !hi);
+    const uint64_t not_fine = __ballot(again);
+    const uint32_t once_more = (uint32_t)(not_fine | not_fine >> 32);   // by column
+    const bool mine = col < n_cols && !(once_more >> at & 1);
     const int oc = mine ? row * p.hq + head : -1;
     if constexpr (S == 1) {
         wait_vm<0>();                          // (tiles without keys: of the first fills)
@@ -465,8 +602,8 @@ __global__ __launch_bounds__(kThreads, DP == 256 || S == 2 ? 1 : 2) void packed_
             for (int e = 0; e < 4; ++e) x[e] = (bf16_t)o_acc[db][4 * r4 + e];
             *reinterpret_cast<bf16x4*>(so + at * kRow + ((db * 4 + r4) ^ k_swz(at)) * 16 + hh * 8) = x;
         }
-    if (hh == 0 && mine && p.lse)
-        p.lse[oc] = hi ? (m2 + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+    if (hh == 0 && col < n_cols && p.lse)
+        p.lse[(int64_t)row * p.hq + head] = hi ? (m2 + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
     int to[CH / 2];
     bf16x8 x[CH / 2];
 #pragma unroll
@@ -479,10 +616,9 @@ __global__ __launch_bounds__(kThreads, DP == 256 || S == 2 ? 1 : 2) void packed_
     for (int i = 0; i < CH / 2; ++i)
         if (to[i] >= 0 && lane % CH * 8 < p.D)
             *reinterpret_cast<bf16x8*>(p.out + (int64_t)to[i] * p.D + lane % CH * 8) = x[i];
-    for (uint32_t left = alone; left; left &= left - 1) {
-        const int c = __builtin_ctz(left);
-        attend_alone<bf16_t, DP>(p, __shfl(row, c), __shfl(head, c), g, __shfl(lo, c), __shfl(hi, c));
-    }
+    if (once_more)
+        attend_again<DP>(p, row, head, g, lo, hi, m2 == -INFINITY ? 0.f : m2, l > 0.f ? 1.f / l : 0.f,
+                         once_more >> at & 1);
 }
 
 // ---- fp32 ----------------------------------------------------------------------------------------
@@ -499,9 +635,6 @@ __global__ __launch_bounds__(kThreads, DP == 256 || S == 2 ? 1 : 2) void packed_
 // many by the bytes that every tile reads from L2 (12 TB/s) and, as much, by the products.  With
 // 16 waves and one workgroup on a CU four of 512 took 21.8 us in place of 10.6, one of 4096 103 and 80.
 constexpr int kF32Waves = 4;
-__device__ __forceinline__ f32x4 mfma_f32(float a, float b, f32x4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
-}
 
 template <int DP, bool WIDE>
 __global__ __launch_bounds__(kF32Waves * 64) void packed_attn_f32_kernel(PackedParams<float> p) {
@@ -654,7 +787,7 @@ __global__ __launch_bounds__(kF32Waves * 64) void packed_attn_f32_kernel(PackedP
                 s_part[(wave * DP + C * (4 * g4 + r) + c) * kColRow + l16] = o_acc[c][r];
     __syncthreads();
     // All columns at once, TPC threads each: of one wave, so that a row of queries that its result replaces is
-    // still there where the column has to be attended alone
+    // still there where the column has to be attended once more
     constexpr int TPC = NW * 64 / 16, EPT = DP / TPC;
     const int cc = tid / TPC, e0 = tid % TPC;
     const int r = s_col[cc][0], h = s_col[cc][1];
@@ -669,7 +802,7 @@ __global__ __launch_bounds__(kF32Waves * 64) void packed_attn_f32_kernel(PackedP
         l += s_l[w][cc] * f[w];
     }
     const float inv = sees ? 1.f / l : 0.f;
-    bool fine = !sees || l < INFINITY;
+    bool fine = true;
 #pragma unroll
     for (int i = 0; i < EPT; ++i) {
         const int d = e0 + i * TPC;
@@ -678,24 +811,31 @@ __global__ __launch_bounds__(kF32Waves * 64) void packed_attn_f32_kernel(PackedP
 #pragma unroll
             for (int w = 0; w < NW; ++w) x[i] += s_part[(w * DP + d) * kColRow + cc] * f[w];
             x[i] *= inv;
-            fine = fine && fabsf(x[i]) < INFINITY;
+            fine = fine && (fabsf(x[i]) < INFINITY || !(l > 0.f));   // weights that are NaN: so is the result
         }
     }
     const uint64_t not_fine = __ballot(!fine && r >= 0);
     const int64_t oc = (int64_t)r * p.hq + h;
-    if (r >= 0 && !(not_fine >> (lane & ~(TPC - 1)) & ((TPC == 64 ? 0 : 1ull << (TPC & 63)) - 1))) {
+    const auto once_more = [&](int c) {    // column c of the wave's
+        return (not_fine >> c * TPC & ((1ull << TPC) - 1)) != 0;
+    };
+    if (r >= 0 && !once_more(lane / TPC)) {
 #pragma unroll
         for (int i = 0; i < EPT; ++i)
             if (WIDE || e0 + i * TPC < D) p.out[oc * D + e0 + i * TPC] = x[i];
-        if (e0 == 0 && p.lse)
-            p.lse[oc] = sees ? (top + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
     }
-    if (not_fine)
-        for (int c = 0; c < 64 / TPC; ++c)
-            if (not_fine >> c * TPC & ((TPC == 64 ? 0 : 1ull << (TPC & 63)) - 1)) {
-                const int* const at = s_col[wave * (64 / TPC) + c];
-                attend_alone<float, DP>(p, at[0], at[1], g, at[2], at[3]);
-            }
+    if (r >= 0 && e0 == 0 && p.lse)
+        p.lse[oc] = sees ? (top + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+    if (not_fine) {
+        constexpr int CPW = 64 / TPC;
+        float mx = -INFINITY, sum_all = 0.f;
+        for (int w = 0; w < NW; ++w) mx = fmaxf(mx, s_m[w][l16]);
+        for (int w = 0; w < NW; ++w)
+            sum_all += s_l[w][l16] * __builtin_amdgcn_exp2f(s_m[w][l16] - (mx == -INFINITY ? 0.f : mx));
+        attend_again_f32<DP>(p, s_col[l16][0], s_col[l16][1], g, s_col[l16][2], s_col[l16][3],
+                             mx == -INFINITY ? 0.f : mx, sum_all > 0.f ? 1.f / sum_all : 0.f,
+                             l16 / CPW == wave && once_more(l16 % CPW));
+    }
 }
 
 template <typename T>
