@@ -23,7 +23,9 @@
 // latter the batch would take 0.6 us less.
 //
 // The reference of a column's exponentials follows the running maximum only when that is 2^8 or more
-// above it: few steps rescale, and the lanes of a column need not meet every step.
+// above it: few steps rescale, and the lanes of a column need not meet every step.  Behind the first
+// scale of 2^65 or more a wave keeps it 2^40 higher still: 2^31 weights of up to 2^8 then sum to no more than
+// the largest value, where they would leave the range before they are divided by their sum.
 //
 // Split.  The keys of a sequence come in groups of kGroup, a step of a workgroup.  One sequence: workgroup j
 // of a kv head takes groups j, j + n_wg, ..: the first one's bytes are on their way before the
@@ -365,7 +367,7 @@ __global__ __launch_bounds__(kWaves * 64) void qcache_attn_kernel(QAttnParams p)
         const bool whole = MULTI ? g == 0 && g_end == groups : p.n_wg == 1;
         const int r_end = min(end_max, (start & ~31) + g_end * kGroup);
 
-        float m2[NC], l[NC];
+        float m2[NC], l[NC], above = 0.f;      // above: by how much the reference is kept over the maximum
         f32x4 o[NC][VB];
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
@@ -420,7 +422,7 @@ __global__ __launch_bounds__(kWaves * 64) void qcache_attn_kernel(QAttnParams p)
                 float top = -INFINITY;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) top = fmaxf(top, sc[c][j >> 2][j & 3]);
-                top *= p.c2;
+                top = fmaf(top, p.c2, above);
                 if (__builtin_expect(__any(top > m2[c] + 8.f), 0)) {
                     float m = fmaxf(top, m2[c]);
                     m = fmaxf(m, __shfl_xor(m, 16));
@@ -442,11 +444,27 @@ __global__ __launch_bounds__(kWaves * 64) void qcache_attn_kernel(QAttnParams p)
                     for (int i = 0; i < PARTS; ++i) pb[c][i][j] = part[i];
                 }
             }
-            // Scale bytes that stand for NaN: their keys count with another scale, and NaN goes into the
-            // columns that see them by a product of its own (0 times NaN would reach the others).
+            // Scale bytes from 192 on: large values, for which the reference rises, and 255, which stands for NaN:
+            // those keys count with another scale, and NaN goes into the columns that see them by a
+            // product of its own (0 times NaN would reach the others).
             u32x2 vs = cur.vs;
-            const u32x2 nan = ((vs & 0x7f7f7f7fu) + 0x01010101u) & vs & 0x80808080u;
-            if (__builtin_expect(__any((nan[0] | nan[1]) != 0), 0)) {
+            const u32x2 large = vs & (vs << 1) & 0x80808080u;
+            if (__builtin_expect(__any((large[0] | large[1]) != 0), 0)) {
+                if (above == 0.f) {
+                    above = 40.f;
+#pragma unroll
+                    for (int c = 0; c < NC; ++c) {
+                        m2[c] += above;
+                        l[c] *= 0x1p-40f;
+#pragma unroll
+                        for (int f = 0; f < VB; ++f) o[c][f] *= 0x1p-40f;
+#pragma unroll
+                        for (int i = 0; i < PARTS; ++i)
+#pragma unroll
+                            for (int j = 0; j < 8; ++j)
+                                pb[c][i][j] = (bf16_t)((float)pb[c][i][j] * 0x1p-40f);
+                    }
+                }
                 bf16x8 is_nan;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
