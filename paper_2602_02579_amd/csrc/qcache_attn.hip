@@ -517,15 +517,6 @@ __global__ __launch_bounds__(kWaves * 64) void qcache_attn_kernel(QAttnParams p)
             const int ahead = r0 + 2 * step;
             load(ahead < r_end ? ahead : r0, t);
         };
-        // Between the last product of a round and what the next one writes first lie as many slots as a result
-        // takes: the compiler, which chains the three parts of a weight through other registers, keeps one
-        // less where a result is only written over.
-        auto end_of_round = [&]() __attribute__((always_inline)) {
-            if constexpr (PARTS > 1) {
-                __builtin_amdgcn_sched_barrier(0);
-                asm volatile("s_nop 1");
-            }
-        };
         if constexpr (TWO_AHEAD) {
             while (r0 + 2 * step < r_end) {
                 load_ahead(t2);
@@ -537,7 +528,6 @@ __global__ __launch_bounds__(kWaves * 64) void qcache_attn_kernel(QAttnParams p)
                 load_ahead(t1);
                 use(r0, t2);
                 r0 += step;
-                end_of_round();
             }
         } else {
             while (r0 + step < r_end) {
@@ -547,7 +537,6 @@ __global__ __launch_bounds__(kWaves * 64) void qcache_attn_kernel(QAttnParams p)
                 use(r0, t1);
                 load_ahead(t1);
                 r0 += step;
-                end_of_round();
             }
         }
         if (r0 < r_end) use(r0, t0);
