@@ -64,12 +64,9 @@ struct QAttnParams {
     float c2;                     // softmax scale * log2(e)
 };
 
-// The cache rows of a sequence from `start` on; row_end: the first one that a row does not see
-__device__ __forceinline__ int start_in_cache(const QAttnParams& p, int start) {
-    return min(max(start, 0), p.rows);
-}
+// The cache rows of a sequence from seq_start on; row_end: the first one that a row does not see
 __device__ __forceinline__ int seq_start(const QAttnParams& p, int s) {
-    return p.seq_start ? start_in_cache(p, p.seq_start[s]) : 0;
+    return p.seq_start ? min(max(p.seq_start[s], 0), p.rows) : 0;
 }
 __device__ __forceinline__ int end_of(const QAttnParams& p, int start, int pos) {
     const int64_t e = (int64_t)start + pos + 1;
@@ -88,12 +85,11 @@ struct Seq {
 };
 __device__ __forceinline__ Seq seq_of(const QAttnParams& p, int s) {
     const int32_t* const row_pos = p.row_pos + (int64_t)s * p.each;
-    const int given = p.seq_start ? p.seq_start[s] : 0;
+    const int start = seq_start(p, s);
     int pos = row_pos[0];
     for (int r = 1; r < p.each; r += 4)       // four at once
 #pragma unroll
         for (int i = 0; i < 4; ++i) pos = max(pos, row_pos[min(r + i, p.each - 1)]);
-    const int start = start_in_cache(p, given);
     return {start, groups_of(start, end_of(p, start, pos))};
 }
 // Several sequences: a workgroup's piece of the line of groups, and the sequence that it is in.  To begin
@@ -307,7 +303,7 @@ __global__ __launch_bounds__(kWaves * 64) void qcache_attn_kernel(QAttnParams p)
     vec_t q_in[NC][F][QV];
     auto request = [&]() __attribute__((always_inline)) {
         s = piece.s;
-        start = MULTI ? piece.seq.start : uniform(p.seq_start ? start_in_cache(p, *p.seq_start) : 0);
+        start = MULTI ? piece.seq.start : uniform(seq_start(p, 0));
         r0 = (start & ~31) + wave * 32 + first_group() * kGroup;
         load(min(r0, p.rows - 32), t0);
         row0 = p.each == 1 ? s : s * p.each + tile0 / p.group;
@@ -671,7 +667,7 @@ __global__ __launch_bounds__(kJoinWaves * 64) void qcache_attn_join_kernel(QAttn
                 x[u][i] = lane + 64 * i < p.D ? p.part_o[at * p.D + lane + 64 * i] : 0.f;
         }
         if (single) {                          // the first workgroup has a part even where there is no key
-            const int start = p.seq_start ? start_in_cache(p, *p.seq_start) : 0;
+            const int start = seq_start(p, 0);
             j1 = min(j_most, max(0, uniform(groups_of(start, row_end(p, start, row))) - 1));
         }
         float mn = m;
