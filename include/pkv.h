@@ -373,7 +373,8 @@ size_t pkv_chunk_attn_workspace_bytes(const pkv_layer_cfg* cfg, int64_t m, int64
  * receives the natural-log normaliser per (row, head).  out may be q itself and overlaps no
  * other operand.  softmax_scale == 0 means 1/sqrt(D).  All tensors 16-byte aligned
  * (PKV_ERR_UNSUPPORTED otherwise, where m * Hq > 2^31 - 1, and in fp32 where m * Hq >= 2^27).
- * Scratch: pkv_packed_attn_workspace_bytes.  m == 0 is a no-op.
+ * The call needs no scratch: pkv_packed_attn_workspace_bytes is 0, and ws and ws_bytes, which it has as the
+ * other calls do, are not looked at.  m == 0 is a no-op.
  */
 pkv_status pkv_packed_attn(const pkv_layer_cfg* cfg,
                            const void* q,          /* [m, Hq, D] */
@@ -662,8 +663,8 @@ pkv_status pkv_layer_rows(const pkv_layer_cfg* cfg, const pkv_layer_call* call, 
 /*
  * The same layer over a packed prompt: the m rows are all of the caches (m == n_cache), dst_row[i] ==
  * i, and attend as pkv_packed_attn says, row_pos counting inside their sequences.  chunk_len must
- * be 0 and score NULL (PKV_ERR_SHAPE otherwise).  Scratch: as for pkv_layer_rows, with
- * pkv_packed_attn_workspace_bytes for the attention.
+ * be 0 and score NULL (PKV_ERR_SHAPE otherwise).  Scratch: as for pkv_layer_rows, of which the attention
+ * takes none.
  */
 pkv_status pkv_layer_rows_packed(const pkv_layer_cfg* cfg, const pkv_layer_call* call,
                                  void* stream);

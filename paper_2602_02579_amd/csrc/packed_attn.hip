@@ -895,11 +895,9 @@ pkv_status launch_f32(PackedParams<float> p, hipStream_t st) {
 
 }  // namespace
 
-size_t packed_attn_ws_bytes(const pkv_layer_cfg&, int64_t) { return 0; }
-
 pkv_status launch_packed_attn(const pkv_layer_cfg& cfg, const void* q, const void* k,
                               const void* v, const int32_t* row_pos, void* out, float* lse_out,
-                              int64_t m, float scale, void*, hipStream_t st) {
+                              int64_t m, float scale, hipStream_t st) {
     const int d = cfg.head_dim;
     if (cfg.dtype == PKV_BF16) {
         const auto p = params<bf16_t>(cfg, q, k, v, row_pos, out, lse_out, m, scale);

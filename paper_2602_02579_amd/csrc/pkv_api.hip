@@ -264,7 +264,7 @@ size_t pkv_chunk_attn_workspace_bytes(const pkv_layer_cfg* cfg, int64_t m, int64
 
 pkv_status pkv_packed_attn(const pkv_layer_cfg* cfg, const void* q, const void* k, const void* v,
                            const int32_t* row_pos, void* out, float* lse_out, int64_t m,
-                           float softmax_scale, void* ws, size_t ws_bytes, void* stream) {
+                           float softmax_scale, void*, size_t, void* stream) {
     pkv_status st = check_cfg(cfg);
     if (st != PKV_OK) return st;
     if (m < 0 || m > kMaxTokens) return PKV_ERR_SHAPE;
@@ -273,19 +273,11 @@ pkv_status pkv_packed_attn(const pkv_layer_cfg* cfg, const void* q, const void* 
     if (m == 0) return PKV_OK;
     if (!q || !k || !v || !row_pos || !out) return PKV_ERR_NULL;
     if (!all_aligned16(q, k, v, out)) return PKV_ERR_UNSUPPORTED;
-    const size_t need = align256(packed_attn_ws_bytes(*cfg, m));
-    if (need && (!ws || ws_bytes < need)) return PKV_ERR_WORKSPACE;
     return launch_packed_attn(*cfg, q, k, v, row_pos, out, lse_out, m,
-                              resolve_scale(softmax_scale, cfg->head_dim), ws,
-                              (hipStream_t)stream);
+                              resolve_scale(softmax_scale, cfg->head_dim), (hipStream_t)stream);
 }
 
-size_t pkv_packed_attn_workspace_bytes(const pkv_layer_cfg* cfg, int64_t m) {
-    if (check_cfg(cfg) != PKV_OK || m <= 0 || m > kMaxTokens ||
-        m * (int64_t)cfg->n_q_heads > INT32_MAX)
-        return 0;
-    return align256(packed_attn_ws_bytes(*cfg, m));
-}
+size_t pkv_packed_attn_workspace_bytes(const pkv_layer_cfg*, int64_t) { return 0; }
 
 pkv_status pkv_qcache_store(const pkv_layer_cfg* cfg, const void* k, const void* v,
                             const int32_t* dst_row, const pkv_qcache* cache, int64_t m,

@@ -140,10 +140,9 @@ pkv_status launch_chunk_attn(const pkv_layer_cfg& cfg, const void* q, const void
                              int64_t chunk_len, float scale, void* ws, hipStream_t st);
 
 // packed_attn.hip
-size_t packed_attn_ws_bytes(const pkv_layer_cfg& cfg, int64_t m);
 pkv_status launch_packed_attn(const pkv_layer_cfg& cfg, const void* q, const void* k,
                               const void* v, const int32_t* row_pos, void* out, float* lse_out,
-                              int64_t m, float scale, void* ws, hipStream_t st);
+                              int64_t m, float scale, hipStream_t st);
 
 // qcache.hip, qcache_attn.hip
 pkv_status launch_qcache_store(const pkv_layer_cfg& cfg, const void* k, const void* v,
