@@ -156,6 +156,8 @@ class Diagnostics:
         length, the last one with what is left, or of the given lengths, which make up the context
         (paragraphs and whole documents are not cut into equal chunks)."""
         n = self.cfg.n_ctx
+        if isinstance(chunk_len, torch.Tensor) and chunk_len.ndim:   # (one length would pass for a number)
+            chunk_len = chunk_len.tolist()
         try:
             chunk_len = operator.index(chunk_len)
         except TypeError:
