@@ -367,12 +367,15 @@ size_t pkv_chunk_attn_workspace_bytes(const pkv_layer_cfg* cfg, int64_t m, int64
  *     out[i, h] = sum_{i - row_pos[i] <= t <= i} softmax_t(q[i,h] . k[t,g(h)] * scale) * v[t, g(h)].
  * A row with row_pos[i] < 0 attends nothing (padding): out 0, lse -inf.  Positions beyond i count
  * as i, so any value is safe; positions that do not begin anew (a window of w rows: min(pos, w - 1))
- * are as good.  fp32 softmax and accumulation, one rounding to cfg->dtype.  Values that are not finite
+ * are as good.  fp32 softmax and accumulation, one rounding to cfg->dtype; in bf16 the weights are rounded
+ * to bf16 before they meet the values (half a step each; their sum is of the unrounded ones), as in
+ * pkv_sparse_row_attn.  Values that are not finite
  * reach the same element of the rows that see them, keys that are not their whole rows, and no
  * others (which costs several times the call without them).  lse_out, if not NULL,
  * receives the natural-log normaliser per (row, head).  out may be q itself and overlaps no
  * other operand.  softmax_scale == 0 means 1/sqrt(D).  All tensors 16-byte aligned
- * (PKV_ERR_UNSUPPORTED otherwise, where m * Hq > 2^31 - 1, and in fp32 where m * Hq >= 2^27).
+ * (PKV_ERR_UNSUPPORTED otherwise, and where m * Hq comes within 256 * Hkv of 2^31, in fp32 within
+ * 16 * Hkv of 2^27, or beyond).
  * The call needs no scratch: pkv_packed_attn_workspace_bytes is 0, and ws and ws_bytes, which it has as the
  * other calls do, are not looked at.  m == 0 is a no-op.
  */
@@ -397,7 +400,7 @@ size_t pkv_packed_attn_workspace_bytes(const pkv_layer_cfg* cfg, int64_t m);
  * head share a scale 2^(byte - 127); an element is 0, 0.5, 1, 1.5, 2, 3, 4 or 6 times it, with a sign:
  * code = 8 * (negative) + index in that list, the element with the even index in the low half of
  * its byte.  pkv_qcache_store writes scale bytes 32 .. 252 and, for 16 elements of which one
- * is not finite, 255: their values are then NaN.
+ * is not finite, 255: their values are then NaN.  Attended rows have these bytes only.
  *
  * The struct is a HOST struct, read during the call; its members are device pointers, 16-byte
  * aligned (PKV_ERR_UNSUPPORTED otherwise).  rows is a positive multiple of 32.  Key and value
@@ -418,7 +421,7 @@ typedef struct {
  * floor(log2(largest magnitude of the 16)) - 2, one more where that magnitude is 7 * 2^e or more,
  * and within the bytes above: the error is at most half the distance of the two values around it.
  * dst_row values must be distinct; rows outside the cache are skipped, no other row is touched.
- * k and v 16-byte aligned.  m == 0 is a no-op.
+ * k and v 16-byte aligned (PKV_ERR_UNSUPPORTED otherwise, and where m * D comes near 2^36).  m == 0 is a no-op.
  */
 pkv_status pkv_qcache_store(const pkv_layer_cfg* cfg,
                             const void* k,          /* [m, Hkv, D] */
@@ -431,8 +434,9 @@ pkv_status pkv_qcache_store(const pkv_layer_cfg* cfg,
  * = row_idx ? row_idx[i] : i and p_i = pos ? pos[i] : pos_base + i: retrieved chunks are put
  * together with their positions, as pkv_rope_restore does for caches in cfg->dtype.  rotate == 0:
  * keys as they were stored (pos is not read).  The stored values are exact in bf16 and fp32; a
- * rotated key is rounded once.  Rows outside the cache are skipped (their output rows stay as
- * they were); the same row may be taken several times.  k_out and v_out 16-byte aligned.
+ * rotated key is rounded once (its sine and cosine are of the angle reduced in fp64, and fp32 themselves).  Rows
+ * outside the cache are skipped (their output rows stay as they were); the same row may be taken
+ * several times.  k_out and v_out 16-byte aligned, m * D as in the store.
  * m == 0 is a no-op.
  */
 pkv_status pkv_qcache_restore(const pkv_layer_cfg* cfg, const pkv_qcache* cache,
@@ -453,7 +457,8 @@ pkv_status pkv_qcache_restore(const pkv_layer_cfg* cfg, const pkv_qcache* cache,
  * cache are never read: a sequence ends where the cache does, and a seq_start outside of 0 .. rows
  * counts as the nearer of these.  Sequences may share rows.
  * q, out and lse_out as in pkv_sparse_row_attn (out may be q itself); 16-byte aligned.  fp32
- * softmax and accumulation, one rounding to cfg->dtype.  Meant for few rows a sequence (up to
+ * softmax and accumulation, one rounding to cfg->dtype, the weights in bf16 as in pkv_packed_attn;
+ * values of the format's whole range.  Meant for few rows a sequence (up to
  * some 64 (row, head of a group) pairs the cache is what is read; beyond, restore it once and use
  * pkv_sparse_row_attn); m * Hq >= 2^23, or 2^20 such pairs of a sequence, is PKV_ERR_UNSUPPORTED.
  * n_seq >= 1 divides m.  Deterministic.  Scratch: pkv_qcache_attn_workspace_bytes.  m == 0 is a no-op.

@@ -11,14 +11,16 @@
 // products run under this one's exponentials.
 //
 // The reference of a column's exponentials follows the running maximum only when that is 2^8 or more
-// above it: most tiles neither rescale nor exchange anything between lanes.
+// above it: most tiles neither rescale nor exchange anything between lanes.  The weights go into the second
+// product in bf16, which is what the matrix instructions take; their sum is of the unrounded ones.  Error against
+// 64 bits 1.3 times that of fp32 weights (the timed cases: 0.0020 of the results' norm and 0.0016).
 //
 // Measured (32 heads on 8, head_dim 128, bf16): seven sequences of 17 to 8192 rows, 23344 together, 1.06 to
 // 1.09 ms, 1.05 to 1.08 PFLOP/s, where a large product of the same box reaches 1.40 and these matrix
 // instructions alone take 774 us: the power limit, then the exponentials (958 us without) and fills (933).
-// Eight of 1 to 512 rows, 2914 together, 28 us (12 to read and write them once): a workgroup's set-up and
+// Eight of 1 to 512 rows, 2914 together, 27.3 us (12 to read and write them once): a workgroup's set-up and
 // results take 9000 of its 28000 clocks.  Few and short ones are a chain of half tiles, 1190 clocks each of
-// which the products are 512; nine of 1 to 512 rows, 1800 together, of 8 heads on 2 take 12.8 us.
+// which the products are 512; nine of 1 to 512 rows, 2000 together, of 8 heads on 2 take 12.9 us.
 #include <atomic>
 #include <type_traits>
 
